@@ -17,6 +17,11 @@ from .binding import (  # noqa: F401
     lora_moe_ws_bytes, lora_moe_apply, lora_moe_apply_static, lora_moe_shrink,
     lora_moe_combine_ws_bytes, lora_moe_down_combine, lora_moe_expand, lora_strerror,
     LORA_DTYPE_BF16, LORA_DTYPE_F32, LORA_MOE_UPGATE, LORA_MOE_DOWN, LORA_ACT_AUTO, LORA_ACT_RESIDENT, LORA_ACT_STREAMING, LORA_MAX_ROWS, LORA_MAX_ROWS_LONG, LORA_STATIC_WS_BYTES,
+    KvCache, KvBatch, KvState, KvMoves, Rope, lora_rope_freqs, lora_rope_append,
+    lora_kv_attention_ws_bytes, lora_kv_attention, lora_kv_moves_ws_bytes, lora_kv_plan, lora_kv_compact, lora_kv_copy_pages,
+    LORA_STATUS_BAD_PAGE, LORA_STATUS_BAD_LENGTH, LORA_STATUS_BAD_SEQ, LORA_STATUS_NO_PAGES, LORA_ROPE_HALF,
+    LORA_ROPE_INTERLEAVED, LORA_ROPE_PLAIN, LORA_ROPE_LINEAR, LORA_ROPE_BASE, LORA_ROPE_PARTS, LORA_KV_MAX_HEAD_DIM,
+    LORA_KV_MAX_PAGE, LORA_KV_MAX_GROUP,
     EXPORTED_SYMBOLS,
     ProvisionError, lora_provision_iar, lora_provision_min_cache, lora_provision_memory_bytes,
 )

@@ -17,6 +17,10 @@ LORA_MAX_PROJ = 8
 LORA_MAX_ROWS = 1 << 14
 LORA_MAX_ROWS_LONG = 1 << 20
 LORA_STATIC_WS_BYTES = 16 << 20
+LORA_STATUS_BAD_PAGE, LORA_STATUS_BAD_LENGTH, LORA_STATUS_BAD_SEQ, LORA_STATUS_NO_PAGES = 4, 8, 16, 32
+LORA_ROPE_HALF, LORA_ROPE_INTERLEAVED = 0, 1
+LORA_ROPE_PLAIN, LORA_ROPE_LINEAR, LORA_ROPE_BASE, LORA_ROPE_PARTS = 0, 1, 2, 3
+LORA_KV_MAX_HEAD_DIM, LORA_KV_MAX_PAGE, LORA_KV_MAX_GROUP = 256, 1024, 64
 
 EXPORTED_SYMBOLS = [
     "lora_strerror", "lora_last_hip_error", "lora_pool_bytes", "lora_register_pool",
@@ -26,6 +30,8 @@ EXPORTED_SYMBOLS = [
     "lora_segments_ws_bytes", "lora_segments_launches", "lora_build_segments", "lora_v_bytes", "lora_shrink",
     "lora_provision_iar", "lora_provision_min_cache", "lora_provision_memory_bytes",
     "lora_expand", "lora_apply", "lora_group_ws_bytes", "lora_group_launches", "lora_apply_group", "lora_build_apply_group", "lora_build_apply_launches", "lora_moe_ws_bytes", "lora_moe_apply", "lora_moe_build_apply", "lora_moe_apply_static", "lora_moe_combine_ws_bytes", "lora_moe_down_combine", "lora_moe_shrink", "lora_moe_expand",
+    "lora_rope_freqs", "lora_rope_append", "lora_kv_attention_ws_bytes", "lora_kv_attention", "lora_kv_moves_ws_bytes",
+    "lora_kv_plan", "lora_kv_compact", "lora_kv_copy_pages",
 ]
 
 
@@ -54,6 +60,39 @@ class _Segments(C.Structure):
                 ("reserved", C.c_int32), ("perm", C.c_void_p),
                 ("seg_start", C.c_void_p), ("seg_key", C.c_void_p), ("tiles", C.c_void_p),
                 ("counts", C.c_void_p), ("status", C.c_void_p)]
+
+
+class _KvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_layers", C.c_int32), ("n_pages", C.c_int32),
+                ("n_heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32), ("reserved", C.c_int32),
+                ("layer_stride", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("token_stride", C.c_int64)]
+
+
+class _KvBatch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32), ("max_pages", C.c_int32),
+                ("row_start", C.c_void_p), ("seq_len", C.c_void_p), ("table", C.c_void_p), ("position", C.c_void_p),
+                ("status", C.c_void_p)]
+
+
+class _RopeDesc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("original_len", C.c_double), ("low", C.c_double), ("high", C.c_double)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int32), ("pairing", C.c_int32), ("amplitude", C.c_float),
+                ("reserved", C.c_int32)]
+
+
+class _KvState(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("table", C.c_void_p), ("seq_len", C.c_void_p),
+                ("page_ref", C.c_void_p)]
+
+
+class _KvMoves(C.Structure):
+    _fields_ = [("capacity", C.c_int32), ("reserved", C.c_int32), ("pairs", C.c_void_p), ("counts", C.c_void_p),
+                ("status", C.c_void_p), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
 
 
 _lib = None
@@ -166,6 +205,25 @@ def load_library():
     lib.lora_provision_min_cache.argtypes = [dp, i32, C.c_double, C.c_double, C.POINTER(C.c_int), dp]
     lib.lora_provision_memory_bytes.restype = C.c_int64
     lib.lora_provision_memory_bytes.argtypes = [i32, C.c_int64]
+    lib.lora_rope_freqs.restype = i32
+    lib.lora_rope_freqs.argtypes = [C.POINTER(_RopeDesc), dp]
+    lib.lora_rope_append.restype = i32
+    lib.lora_rope_append.argtypes = [C.POINTER(_KvCache), i32, C.POINTER(_KvBatch), C.POINTER(_Rope), vp, i64, vp, i64, vp,
+                                     i64, vp, i64, i32, i32, vp]
+    lib.lora_kv_attention_ws_bytes.restype = sz
+    lib.lora_kv_attention_ws_bytes.argtypes = [C.POINTER(_KvCache), C.POINTER(_KvBatch), i32]
+    lib.lora_kv_attention.restype = i32
+    lib.lora_kv_attention.argtypes = [C.POINTER(_KvCache), i32, C.POINTER(_KvBatch), vp, i64, i32, vp, i64, vp, C.c_float,
+                                      i32, i32, vp, sz, vp]
+    lib.lora_kv_moves_ws_bytes.restype = sz
+    lib.lora_kv_moves_ws_bytes.argtypes = [i32, i32]
+    lib.lora_kv_plan.restype = i32
+    lib.lora_kv_plan.argtypes = [C.POINTER(_KvCache), C.POINTER(_KvState), C.POINTER(_KvState), vp, vp,
+                                 C.POINTER(_KvMoves), vp]
+    lib.lora_kv_compact.restype = i32
+    lib.lora_kv_compact.argtypes = [C.POINTER(_KvCache), C.POINTER(_KvState), C.POINTER(_KvState), C.POINTER(_KvMoves), vp]
+    lib.lora_kv_copy_pages.restype = i32
+    lib.lora_kv_copy_pages.argtypes = [C.POINTER(_KvCache), C.POINTER(_KvMoves), i32, vp]
     global _pycall
     if not os.path.exists(os.path.join(os.path.dirname(path), "_pycall.so")):
         raise RuntimeError("_pycall.so is not built; run `python -m paper_2604_07173_amd.build`")
@@ -525,6 +583,128 @@ def lora_moe_down_combine(pool, layer, hmid, ld_in, adapter_id, expert_id, seg: 
                                    ldy, ws, ws_bytes, stream)
     if rc:
         _check(rc, "lora_moe_down_combine")
+
+
+# ---- paged cache (include/lora_attn.h) ---------------------------------------------------------
+
+
+class KvCache:
+    """lora_kv_cache over two tensors seen as [layer][page][head][token][width], in any order in memory
+    (bf16, the same strides, the width contiguous).  Holds the tensors."""
+
+    def __init__(self, k, v):
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.stride(4) != 1 or k.element_size() != 2 \
+                or v.element_size() != 2:
+            raise ValueError("k and v: [layer][page][head][token][width] of 16 bits, alike in shape and strides")
+        self.k, self.v = k, v
+        c = self.c = _KvCache()
+        c.k, c.v = k.data_ptr(), v.data_ptr()
+        c.n_layers, c.n_pages, c.n_heads, c.page_size, c.head_dim = k.shape
+        c.layer_stride, c.page_stride, c.head_stride, c.token_stride = k.stride()[:4]
+
+
+def _int32(t, what, shape):
+    if t.element_size() != 4 or t.is_floating_point() or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: a contiguous int32 tensor {list(shape)}, got {t.dtype} {list(t.shape)}")
+    return t
+
+
+class KvBatch:
+    """lora_kv_batch over int32 device tensors: row_start [n_seqs + 1], seq_len [n_seqs], table
+    [n_seqs][max_pages], position [n_rows] or None.  Holds the tensors and a status word."""
+
+    def __init__(self, row_start, seq_len, table, n_rows: int, max_rows: int = 0, position=None, status=None):
+        import torch
+        n = seq_len.shape[0]
+        self.row_start, self.seq_len = _int32(row_start, "row_start", (n + 1,)), _int32(seq_len, "seq_len", (n,))
+        self.table = _int32(table, "table", (n, table.shape[-1]))
+        self.position = None if position is None else _int32(position, "position", (n_rows,))
+        self.status = torch.zeros(1, dtype=torch.int32, device=seq_len.device) if status is None else status
+        c = self.c = _KvBatch()
+        c.n_seqs, c.n_rows, c.max_rows, c.max_pages = n, int(n_rows), int(max_rows), table.shape[1]
+        c.row_start, c.seq_len, c.table = row_start.data_ptr(), seq_len.data_ptr(), table.data_ptr()
+        c.position, c.status = _addr(position), self.status.data_ptr()
+
+
+def lora_rope_freqs(rot_dim: int, base: float = 10000.0, scaling: int = LORA_ROPE_PLAIN, factor: float = 1.0,
+                    original_len: float = 0.0, low: float = 1.0, high: float = 32.0) -> list:
+    """Radians per position of the rot_dim / 2 pairs (host)."""
+    d = _RopeDesc(rot_dim, scaling, base, factor, original_len, low, high)
+    out = (C.c_double * max(rot_dim // 2, 1))()
+    _check(load_library().lora_rope_freqs(C.byref(d), out), "lora_rope_freqs")
+    return list(out)
+
+
+class Rope:
+    """lora_rope with its frequencies on the device (the arguments of lora_rope_freqs)."""
+
+    def __init__(self, rot_dim: int, pairing: int = LORA_ROPE_HALF, amplitude: float = 1.0, device="cuda", **scaling):
+        import torch
+        self.freq = torch.tensor(lora_rope_freqs(rot_dim, **scaling), dtype=torch.float64).to(device)
+        self.c = _Rope(self.freq.data_ptr(), rot_dim, pairing, amplitude, 0)
+
+
+def _c(handle):
+    return None if handle is None else C.byref(handle.c)
+
+
+def lora_rope_append(cache: KvCache, layer: int, batch: KvBatch, rope: Optional[Rope], q, ldq, k, ldk, v, ldv, q_out, ldqo,
+                     n_heads: int, in_dtype=LORA_DTYPE_BF16, stream=None):
+    _check(load_library().lora_rope_append(_c(cache), layer, _c(batch), _c(rope), _addr(q), ldq, _addr(k), ldk, _addr(v), ldv,
+                                           _addr(q_out), ldqo, n_heads, in_dtype, _stream(stream)), "lora_rope_append")
+
+
+def lora_kv_attention_ws_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int:
+    return int(load_library().lora_kv_attention_ws_bytes(_c(cache), _c(batch), n_heads))
+
+
+def lora_kv_attention(cache: KvCache, layer: int, batch: KvBatch, q, ldq, n_heads: int, out, ldo, lse, scale: float, ws,
+                      causal: bool = True, window: int = 0, stream=None):
+    _check(load_library().lora_kv_attention(_c(cache), layer, _c(batch), _addr(q), ldq, n_heads, _addr(out), ldo, _addr(lse),
+                                            scale, int(causal), window, _addr(ws), ws.numel() * ws.element_size(),
+                                            _stream(stream)), "lora_kv_attention")
+
+
+def lora_kv_moves_ws_bytes(n_pages: int, n_seqs: int) -> int:
+    return int(load_library().lora_kv_moves_ws_bytes(n_pages, n_seqs))
+
+
+class KvState:
+    """lora_kv_state over int32 device tensors: table [n_seqs][max_pages], seq_len [n_seqs], page_ref [n_pages]."""
+
+    def __init__(self, table, seq_len, page_ref=None):
+        n = seq_len.shape[0]
+        self.table, self.seq_len = _int32(table, "table", (n, table.shape[-1])), _int32(seq_len, "seq_len", (n,))
+        self.page_ref = None if page_ref is None else _int32(page_ref, "page_ref", (page_ref.shape[0],))
+        self.c = _KvState(n, table.shape[1], table.data_ptr(), seq_len.data_ptr(), _addr(page_ref))
+
+
+class KvMoves:
+    """Device buffers of a lora_kv_moves for plans of n_seqs slots and compactions of n_pages pages."""
+
+    def __init__(self, n_pages: int, n_seqs: int, device="cuda"):
+        import torch
+        capacity = max(n_seqs, n_pages // 2, 1)
+        self.pairs = torch.empty((capacity, 2), dtype=torch.int32, device=device)
+        self.counts = torch.zeros(4, dtype=torch.int32, device=device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.ws = torch.empty(max(lora_kv_moves_ws_bytes(n_pages, n_seqs), 256), dtype=torch.uint8, device=device)
+        self.c = _KvMoves(capacity, 0, self.pairs.data_ptr(), self.counts.data_ptr(), self.status.data_ptr(),
+                          self.ws.data_ptr(), self.ws.numel())
+
+
+def lora_kv_plan(cache: KvCache, state: KvState, to: KvState, src, new_len, moves: KvMoves, stream=None):
+    """src, new_len: int32 device tensors [n_seqs]."""
+    _check(load_library().lora_kv_plan(_c(cache), _c(state), _c(to), _addr(src), _addr(new_len), _c(moves), _stream(stream)),
+           "lora_kv_plan")
+
+
+def lora_kv_compact(cache: KvCache, state: KvState, to: KvState, moves: KvMoves, stream=None):
+    _check(load_library().lora_kv_compact(_c(cache), _c(state), _c(to), _c(moves), _stream(stream)), "lora_kv_compact")
+
+
+def lora_kv_copy_pages(cache: KvCache, moves: KvMoves, max_moves: int, stream=None):
+    _check(load_library().lora_kv_copy_pages(_c(cache), _c(moves), max_moves, _stream(stream)), "lora_kv_copy_pages")
 
 
 # ---- cache provisioning (include/lora_provision.h): host arrays in, numbers out ----------------

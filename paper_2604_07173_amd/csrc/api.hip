@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "adapter_ranks.h"
+#include "kv_internal.h"
 #include "lora_internal.h"
 
 using namespace lora;
@@ -773,6 +774,13 @@ int check_act(const void *ptr, int64_t ld, int width, size_t elem)
 }
 
 }  // namespace
+
+namespace lora {
+
+// for the entry points outside this file: the text that lora_last_hip_error gives
+int note_hip_error(hipError_t e) { return hip_fail(e); }
+
+}  // namespace lora
 
 extern "C" {
 

@@ -1,0 +1,34 @@
+// Device-side helpers of the paged cache.
+#pragma once
+#include "kv_internal.h"
+#include "lora_device.h"
+
+namespace lora {
+
+// Last index i of a non-decreasing array a[0 .. n) with a[i] <= x, found by a whole wave: 64 values are
+// compared at a time, so up to 64 entries take one load and up to 4096 two.  a[0] <= x is taken for granted.
+__device__ inline int wave_find(const int32_t *a, int n, int x)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0;
+    while (n > 1) {
+        const int step = (n + 63) >> 6;
+        const int i = lane * step;
+        const bool le = i < n && a[lo + min(i, n - 1)] <= x;
+        const int k = max(0, (int)__popcll(__ballot(le)) - 1);
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return lo;
+}
+
+// Page of a token by its table entry; an entry that is no page of the cache raises the status bit and is
+// replaced by a page that is, so that nothing is read out of bounds.
+__device__ inline int checked_page(int page, int n_pages, uint32_t *status)
+{
+    if ((unsigned)page < (unsigned)n_pages) return page;
+    atomicOr(status, LORA_STATUS_BAD_PAGE);
+    return 0;
+}
+
+}  // namespace lora

@@ -1,0 +1,316 @@
+"""lora_kv_plan, lora_kv_compact and lora_kv_copy_pages against a bookkeeper written with lists and sets."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_07173_amd as L
+
+pytestmark = pytest.mark.gpu
+
+
+class Books:
+    """The state on the host: a list of pages per slot, and what every place of every page holds."""
+
+    def __init__(self, n_pages, n_slots, page, max_pages):
+        self.n_pages, self.page, self.max_pages = n_pages, page, max_pages
+        self.pages = [[] for _ in range(n_slots)]
+        self.len = [0] * n_slots
+
+    def ref(self):
+        r = np.zeros(self.n_pages, np.int32)
+        for p in self.pages:
+            for x in p:
+                r[x] += 1
+        return r
+
+    def plan(self, src, new):
+        """The next state, its copies and the pages asked for; None in the state's place if they are not there."""
+        page = self.page
+        nxt = Books(self.n_pages, len(src), page, self.max_pages)
+        keep = [min(self.len[p], n) if p >= 0 else 0 for p, n in zip(src, new)]
+        kept = [self.pages[p][:-(-k // page)] if p >= 0 else [] for p, k in zip(src, keep)]
+        holders = {}
+        for s, pages in enumerate(kept):
+            for x in pages:
+                holders.setdefault(x, []).append(s)
+        grows = [n > k and k % page > 0 for k, n in zip(keep, new)]
+        need, copies = [], []
+        for s in range(len(src)):
+            cow = False
+            if grows[s]:
+                all_ = holders[kept[s][-1]]
+                writers = [u for u in all_ if grows[u] and kept[u][-1] == kept[s][-1]]
+                cow = len(all_) > 1 and not (len(writers) == len(all_) and min(writers) == s)
+            need.append(cow + -(-new[s] // page) - len(kept[s]))
+            copies.append(cow)
+        free = sorted(set(range(self.n_pages)) - set(holders))
+        if sum(need) > len(free):
+            return None, [], sum(need)
+        pairs = []
+        for s in range(len(src)):
+            pages = list(kept[s])
+            if copies[s]:
+                mine = free.pop(0)
+                pairs.append((pages[-1], mine))
+                pages[-1] = mine
+            while len(pages) < -(-new[s] // page):
+                pages.append(free.pop(0))
+            nxt.pages[s], nxt.len[s] = pages, new[s]
+        return nxt, pairs, sum(need)
+
+    def compact(self):
+        live = sorted({x for p in self.pages for x in p})
+        holes = sorted(set(range(len(live))) - set(live))
+        movers = [x for x in live if x >= len(live)]
+        to = dict(zip(movers, holes))
+        nxt = Books(self.n_pages, len(self.len), self.page, self.max_pages)
+        nxt.pages = [[to.get(x, x) for x in p] for p in self.pages]
+        nxt.len = list(self.len)
+        return nxt, list(zip(movers, holes)), 0
+
+    def table(self):
+        t = np.full((len(self.len), self.max_pages), -1, np.int32)
+        for s, p in enumerate(self.pages):
+            t[s, :len(p)] = p
+        return t
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+
+def state_of(books, with_ref=True):
+    return L.KvState(dev(books.table()), dev(books.len), dev(books.ref()) if with_ref else None)
+
+
+def blank(books):
+    n = len(books.len)
+    return L.KvState(dev(np.full((n, books.max_pages), -9)), dev(np.full(n, -9)), dev(np.full(books.n_pages, -9)))
+
+
+def cache_of(n_pages, page, layers=2, kv=2, dim=8):
+    k, v = (torch.randn((layers, n_pages, kv, page, dim), device="cuda").bfloat16() for _ in range(2))
+    return L.KvCache(k, v)
+
+
+def check(books, state, moves, pairs, wanted):
+    assert np.array_equal(state.table.cpu().numpy(), books.table())
+    assert state.seq_len.cpu().tolist() == books.len
+    ref = books.ref()
+    assert np.array_equal(state.page_ref.cpu().numpy(), ref)
+    used = int((ref > 0).sum())
+    assert moves.counts.cpu().tolist() == [used, len(pairs), books.n_pages - used, wanted]
+    assert [tuple(p) for p in moves.pairs.cpu().tolist()[:len(pairs)]] == pairs
+    assert int(moves.status.item()) == 0
+
+
+@pytest.mark.parametrize("page", [1, 4, 16])
+@pytest.mark.parametrize("n_slots,n_pages", [(1, 5), (7, 40), (64, 700), (65, 3000), (1500, 5000)])
+def test_a_run_of_plans(page, n_slots, n_pages):
+    """Growth, ends, falls back and forks at random, step after step, with a compaction now and then."""
+    rng = np.random.default_rng(n_slots + page)
+    max_pages = min(n_pages, 12)
+    books = Books(n_pages, n_slots, page, max_pages)
+    cache = cache_of(n_pages, page)
+    moves = L.KvMoves(n_pages, n_slots)
+    state = state_of(books)
+    refused = 0
+    for step in range(14):
+        if step % 5 == 4:
+            nxt, pairs, wanted = books.compact()
+            to = blank(books)
+            L.lora_kv_compact(cache, state, to, moves)
+        else:
+            src = np.where(rng.random(n_slots) < 0.7, np.arange(n_slots), rng.integers(-1, n_slots, n_slots))
+            had = np.array([books.len[s] if s >= 0 else 0 for s in src])
+            new = had + rng.integers(0, 3 * page + 2, n_slots)
+            fall = rng.random(n_slots)
+            new = np.where(fall < 0.15, 0, np.where(fall < 0.3, rng.integers(0, had + 1), new))
+            new = np.minimum(new, max_pages * page)
+            nxt, pairs, wanted = books.plan(src.tolist(), new.tolist())
+            to = blank(books)
+            L.lora_kv_plan(cache, state, to, dev(src), dev(new), moves)
+        torch.cuda.synchronize()
+        if nxt is None:
+            refused += 1
+            assert int(moves.status.item()) == L.LORA_STATUS_NO_PAGES
+            assert torch.equal(to.table, state.table) and torch.equal(to.seq_len, state.seq_len)
+            assert torch.equal(to.page_ref, state.page_ref)
+            assert moves.counts.cpu().tolist() == [0, 0, 0, wanted]
+            moves.status.zero_()
+            continue
+        check(nxt, to, moves, pairs, wanted)
+        want_k, want_v = cache.k.clone(), cache.v.clone()
+        for a, b in pairs:
+            want_k[:, b], want_v[:, b] = cache.k[:, a], cache.v[:, a]
+        L.lora_kv_copy_pages(cache, moves, max_moves=max(n_slots, n_pages // 2))
+        torch.cuda.synchronize()
+        assert torch.equal(cache.k, want_k) and torch.equal(cache.v, want_v)
+        books, state = nxt, to
+
+
+def test_forks_share_and_copy_on_write():
+    books = Books(20, 4, 4, 5)
+    books.pages[0], books.len[0] = [7, 3], 6                   # one page full, one half full
+    cache, moves = cache_of(20, 4), L.KvMoves(20, 4)
+    for src, new, copies in (
+            ([0, 0, 0, -1], [6, 6, 6, 0], 0),                   # shared, nobody writes
+            ([0, 0, 0, -1], [7, 7, 7, 0], 2),                   # everybody writes: the first keeps the page
+            ([0, 0, 0, -1], [6, 7, 7, 0], 2),                   # the first one reads on: two copies
+            ([0, 0, 0, -1], [7, 3, 7, 0], 1),                   # one fell back into the full page
+            ([-1, 0, -1, 0], [2, 5, 0, 9], 1),                  # one fell back inside the page, one grows there and beyond
+            ([0, 0, 0, 0], [8, 9, 4, 0], 1)):
+        nxt, pairs, wanted = books.plan(src, new)
+        assert len(pairs) == copies
+        to = blank(books)
+        L.lora_kv_plan(cache, state_of(books, False), to, dev(src), dev(new), moves)
+        torch.cuda.synchronize()
+        check(nxt, to, moves, pairs, wanted)
+
+
+def test_without_page_ref():
+    books = Books(20, 2, 4, 5)
+    books.pages[0], books.len[0] = [7, 3], 6
+    cache, moves = cache_of(20, 4), L.KvMoves(20, 2)
+    to = blank(books)
+    to.c.page_ref = None
+    L.lora_kv_plan(cache, state_of(books, False), to, dev([0, 0]), dev([7, 8]), moves)
+    torch.cuda.synchronize()
+    nxt, pairs, _ = books.plan([0, 0], [7, 8])
+    assert np.array_equal(to.table.cpu().numpy(), nxt.table()) and (to.page_ref == -9).all()
+    to = blank(books)
+    to.c.page_ref = None
+    L.lora_kv_compact(cache, state_of(books, False), to, moves)
+    torch.cuda.synchronize()
+    assert np.array_equal(to.table.cpu().numpy(), books.compact()[0].table()) and (to.page_ref == -9).all()
+
+
+@pytest.mark.parametrize("src,new,bit", [([0, 2], [3, 3], L.LORA_STATUS_BAD_SEQ), ([0, -2], [3, 3], L.LORA_STATUS_BAD_SEQ),
+                                         ([0, 1], [3, -1], L.LORA_STATUS_BAD_LENGTH), ([0, 1], [21, 0], L.LORA_STATUS_BAD_LENGTH),
+                                         ([1, 1], [5, 0], L.LORA_STATUS_BAD_PAGE)])
+def test_plans_that_make_no_sense_change_nothing(src, new, bit):
+    books = Books(20, 2, 4, 5)
+    books.pages, books.len = [[7, 3], [5, 6]], [6, 8]
+    state = state_of(books)
+    if bit == L.LORA_STATUS_BAD_PAGE:
+        state.table[1, 1] = 20
+    cache, moves, to = cache_of(20, 4), L.KvMoves(20, 2), blank(books)
+    L.lora_kv_plan(cache, state, to, dev(src), dev(new), moves)
+    torch.cuda.synchronize()
+    assert int(moves.status.item()) == bit
+    assert torch.equal(to.table, state.table) and torch.equal(to.seq_len, state.seq_len) and torch.equal(to.page_ref, state.page_ref)
+    assert moves.counts.cpu().tolist() == [0, 0, 0, 0]
+
+
+def test_compaction_of_a_broken_table_changes_nothing():
+    books = Books(20, 2, 4, 5)
+    books.pages, books.len = [[7, 3], [5, 6]], [6, 8]
+    state = state_of(books)
+    state.table[0, 0] = -3
+    cache, moves, to = cache_of(20, 4), L.KvMoves(20, 2), blank(books)
+    L.lora_kv_compact(cache, state, to, moves)
+    torch.cuda.synchronize()
+    assert int(moves.status.item()) == L.LORA_STATUS_BAD_PAGE
+    assert torch.equal(to.table, state.table) and torch.equal(to.page_ref, state.page_ref)
+
+
+@pytest.mark.parametrize("n_pages,held", [(1, 1), (1, 0), (2, 1), (1024, 500), (1025, 1025), (2049, 1024), (9000, 4500), (9000, 1)])
+def test_compaction(n_pages, held):
+    rng = np.random.default_rng(n_pages + held)
+    slots = 9
+    books = Books(n_pages, slots, 2, max(1, held))
+    order = rng.permutation(n_pages)[:held].tolist()
+    for i, x in enumerate(order):
+        books.pages[i % slots].append(x)
+    if held > 20:
+        books.pages[1] = books.pages[0][:5] + books.pages[1]          # shared pages
+    books.len = [max(0, 2 * len(p) - 1) for p in books.pages]
+    cache, moves, to = cache_of(n_pages, 2), L.KvMoves(n_pages, slots), blank(books)
+    L.lora_kv_compact(cache, state_of(books), to, moves)
+    torch.cuda.synchronize()
+    nxt, pairs, _ = books.compact()
+    check(nxt, to, moves, pairs, 0)
+    want = cache.k.clone()
+    for a, b in pairs:
+        want[:, b] = cache.k[:, a]
+    if n_pages > 1:
+        L.lora_kv_copy_pages(cache, moves, n_pages // 2)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.k, want)
+
+
+@pytest.mark.parametrize("order", ["head", "token", "layers_inside", "holes", "heads_apart"])
+@pytest.mark.parametrize("kv,page,dim", [(2, 16, 64), (1, 8, 40), (5, 32, 80), (8, 1, 128), (3, 64, 256)])
+def test_copies_of_every_layout(order, kv, page, dim):
+    layers, n = 3, 11
+    both = []
+    for _ in range(2):
+        if order == "head":
+            t = torch.randn((layers, n, kv, page, dim), device="cuda").bfloat16()
+        elif order == "token":
+            t = torch.randn((layers, n, page, kv, dim), device="cuda").bfloat16().transpose(2, 3)
+        elif order == "layers_inside":
+            t = torch.randn((n, layers, kv, page, dim), device="cuda").bfloat16().transpose(0, 1)
+        elif order == "holes":
+            t = torch.randn((layers, n, kv, page, dim + 8), device="cuda").bfloat16()[..., :dim]
+        else:
+            t = torch.randn((layers, n, kv, page + 1, dim), device="cuda").bfloat16()[:, :, :, :page]
+        both.append(t)
+    cache, moves = L.KvCache(*both), L.KvMoves(n, 4)
+    pairs = [(3, 0), (9, 2), (3, 8), (10, 1)]
+    moves.pairs[:4] = dev(pairs)
+    moves.counts[1] = 3                                    # the fourth is not asked for
+    want = [t.clone() for t in both]
+    for w in want:
+        for a, b in pairs[:3]:
+            w[:, b] = w[:, a]
+    base = [t._base.clone() if t._base is not None else t for t in both]
+    L.lora_kv_copy_pages(cache, moves, max_moves=4)
+    torch.cuda.synchronize()
+    for t, w, b in zip(both, want, base):
+        assert torch.equal(t, w)
+        if order == "holes":
+            assert torch.equal(t._base[..., dim:], b[..., dim:])
+        if order == "heads_apart":
+            assert torch.equal(t._base[:, :, :, page:], b[:, :, :, page:])
+    L.lora_kv_copy_pages(cache, moves, max_moves=0)
+
+
+def test_no_more_moves_than_the_bound():
+    cache, moves = cache_of(8, 4), L.KvMoves(8, 4)
+    moves.pairs[:3] = dev([(0, 4), (1, 5), (2, 6)])
+    moves.counts[1] = 3
+    want = cache.k.clone()
+    want[:, 4] = want[:, 0]
+    L.lora_kv_copy_pages(cache, moves, max_moves=1)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.k, want)
+
+
+def test_in_a_graph():
+    """A plan and its copies, replayed with other lengths between eager work of the program."""
+    books = Books(40, 5, 4, 8)
+    books.pages, books.len = [[30, 2], [9], [4, 5, 6], [], [1]], [7, 3, 12, 0, 4]
+    cache, moves = cache_of(40, 4), L.KvMoves(40, 5)
+    state, to = state_of(books), blank(books)
+    src, new = dev([0, 1, 2, 0, 4]), dev([8, 4, 13, 9, 5])
+
+    def call():
+        L.lora_kv_plan(cache, state, to, src, new, moves)
+        L.lora_kv_copy_pages(cache, moves, 5)
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for s, n in (([0, 1, 2, 0, 4], [8, 4, 13, 9, 5]), ([4, 4, 4, 4, 4], [4, 5, 6, 7, 8]), ([-1, 0, 0, 1, 2], [3, 8, 7, 9, 0])):
+        src.copy_(dev(s))
+        new.copy_(dev(n))
+        nxt, pairs, wanted = books.plan(s, n)
+        want = cache.k.clone()
+        for a, b in pairs:
+            want[:, b] = want[:, a]
+        g.replay()
+        torch.cuda.synchronize()
+        check(nxt, to, moves, pairs, wanted)
+        assert torch.equal(cache.k, want)
