@@ -12,10 +12,12 @@
 // P as the result of the first product hold it as the operand of the second: the 32 tokens go into
 // the second product in the order in which the first left them (group g: tokens 4g .. 4g+3 and
 // 16+4g .. 16+4g+3).  V is read transposed from LDS in that order (ds_read_b64_tr_b16).
+#include <limits.h>
+
 #include <algorithm>
 #include <cmath>
 
-#include "kv_device.h"
+#include "kv_attention.h"
 
 namespace lora {
 
@@ -23,135 +25,99 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kBlock = 32;               // tokens of a wave's step
-constexpr int kRows = 16;                // rows of a tile
-constexpr int kMinSplit = 256;           // tokens of a work item at least, where a range is cut
-constexpr int kTargetItems = 2048;       // work items that fill the chip
+constexpr int kRows = kShortTile;
 constexpr int kPlanThreads = 1024;
-constexpr float kLn2 = 0.6931471805599453f;
 
-// Device plan: plan[0] = tokens of a work item's range, plan[1 + s] = work items before sequence s.
-struct Seq {
-    int rows, len, pos0;                 // new rows, length, position of the first new row
-};
-
-__device__ inline Seq seq_of(const KvRows &b, int s)
-{
-    Seq q;
-    const int first = min(max(0, b.row_start[s]), b.n_rows);
-    q.rows = max(0, min(b.row_start[s + 1], b.n_rows) - first);
-    q.len = min(max(0, b.seq_len[s]), b.tokens_max);
-    q.pos0 = q.len - q.rows;
-    return q;
-}
-
-__device__ inline int tiles_of(const Seq &q, int group) { return (q.rows * group + kRows - 1) / kRows; }
-
-// Most tokens that a tile of the sequence sees.
-__device__ inline int reach_of(const AttnParams &p, const Seq &q)
-{
-    if (!p.window) return q.len;
-    const int64_t most = (int64_t)p.window - 1 + min(q.rows, kRows / p.group + 2);
-    return (int)min((int64_t)q.len, most);
-}
-
-__device__ inline int splits_of(int reach, int chunk) { return max(1, (reach + chunk - 1) / chunk); }
-
-// Cuts the ranges so that all work items take about as long, at most max_items of them.
+// Cuts the ranges so that all work items of a kind take about as long.
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
 {
-    __shared__ int64_t s_sum[kPlanThreads / 64];
+    constexpr int WAVES = kPlanThreads / 64;
+    __shared__ int64_t s_work[2][WAVES];
+    __shared__ int s_sum[4][WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t work = 0;
+    int64_t work[2] = {0, 0};
     unsigned bad = 0;
     for (int s = threadIdx.x; s < p.b.n_seqs; s += kPlanThreads) {
         const Seq q = seq_of(p.b, s);
-        if (p.b.seq_len[s] != q.len) bad = 1;
-        work += (int64_t)tiles_of(q, p.group) * reach_of(p, q);
+        if (p.b.seq_len[s] != q.len) bad |= 1;
+        const int first = p.b.row_start[s], end = p.b.row_start[s + 1];
+        if (first < 0 || end < first || end > p.b.n_rows || (s == 0 && first != 0) || (s == p.b.n_seqs - 1 && end != p.b.n_rows)) bad |= 2;
+        work[0] += (int64_t)tiles_of<kShortTile>(p, q) * reach_of<kShortTile>(p, q);
+        work[1] += (int64_t)tiles_of<kLongTile>(p, q) * reach_of<kLongTile>(p, q);
     }
     if (bad) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d);
-    if (lane == 0) s_sum[wave] = work;
-    __syncthreads();
-    work = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) work += s_sum[w];
-    const int64_t each = (work * p.c.n_heads + kTargetItems - 1) / kTargetItems;
-    const int chunk = (int)min(((max(each, (int64_t)kMinSplit) + 127) >> 7) << 7, (int64_t)1 << 30);
-    int base = 0;
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int d = 32; d; d >>= 1) work[k] += __shfl_xor(work[k], d);
+        if (lane == 0) s_work[k][wave] = work[k];
+    }
+    const bool no_rows = __syncthreads_or(bad & 2);      // rows that are no partition: nothing is computed
+    int chunk[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        int64_t all = 0;
+        for (int w = 0; w < WAVES; ++w) all += s_work[k][w];
+        const int64_t target = k ? kLongTarget : kShortTarget, least = k ? kLongMinSplit : kShortMinSplit;
+        const int64_t each = (all * p.c.n_heads + target - 1) / target;
+        chunk[k] = (int)min(((max(each, least) + 127) >> 7) << 7, (int64_t)1 << 30);
+    }
+    int32_t *array = p.plan + kPlanHead;
+    int base[4] = {0, 0, 0, 0};
     for (int s0 = 0; s0 < p.b.n_seqs; s0 += kPlanThreads) {
         const int s = s0 + threadIdx.x;
-        int items = 0;
+        int own[4] = {0, 0, 0, 0}, v[4];
         if (s < p.b.n_seqs) {
             const Seq q = seq_of(p.b, s);
-            items = tiles_of(q, p.group) * splits_of(reach_of(p, q), chunk) * p.c.n_heads;
+            const int cut_s = splits_of(reach_of<kShortTile>(p, q), chunk[0]), cut_l = splits_of(reach_of<kLongTile>(p, q), chunk[1]);
+            own[0] = tiles_of<kShortTile>(p, q) * cut_s * p.c.n_heads;
+            own[1] = cut_s > 1 ? own[0] : 0;
+            own[2] = tiles_of<kLongTile>(p, q) * cut_l * p.c.n_heads;
+            own[3] = cut_l > 1 ? own[2] : 0;
         }
-        int v = items;
+        __syncthreads();
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(v, d);
-            if (lane >= d) v += o;
+        for (int k = 0; k < 4; ++k) {
+            v[k] = own[k];
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(v[k], d);
+                if (lane >= d) v[k] += o;
+            }
+            if (lane == 63) s_sum[k][wave] = v[k];
         }
         __syncthreads();
-        if (lane == 63) s_sum[wave] = v;
-        __syncthreads();
-        int total = 0;
-        for (int w = 0; w < kPlanThreads / 64; ++w) {
-            if (w < wave) v += (int)s_sum[w];
-            total += (int)s_sum[w];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            int total = 0;
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) v[k] += s_sum[k][w];
+                total += s_sum[k][w];
+            }
+            if (s < p.b.n_seqs) array[(int64_t)k * p.b.n_seqs + s] = base[k] + v[k] - own[k];
+            base[k] += total;
         }
-        if (s < p.b.n_seqs) p.plan[1 + s] = base + v - items;
-        base += total;
     }
     if (threadIdx.x == 0) {
-        p.plan[0] = chunk;
-        p.plan[1 + p.b.n_seqs] = base;
+        p.plan[kChunkShort] = no_rows ? INT_MAX : chunk[0];
+        p.plan[kChunkLong] = no_rows ? INT_MAX : chunk[1];
+        p.plan[kItemsShort] = no_rows ? 0 : base[0];
+        p.plan[kItemsLong] = no_rows ? 0 : base[2];
     }
 }
 
-// A tile's tokens: [lo, hi), and of them the part of one of its splits.
-struct Range {
-    int lo, hi, splits;
-};
-
-__device__ inline Range range_of(const AttnParams &p, const Seq &q, int tile, int chunk)
-{
-    const int i0 = tile * kRows / p.group, i1 = min(q.rows - 1, (tile * kRows + kRows - 1) / p.group);
-    Range r;
-    r.hi = p.causal ? max(0, min(q.len, q.pos0 + i1 + 1)) : q.len;
-    r.lo = p.window ? max(0, q.pos0 + i0 - p.window + 1) : 0;
-    if (r.lo >= r.hi) r.lo = r.hi = 0;
-    r.splits = splits_of(r.hi - r.lo, chunk);
-    return r;
-}
-
-// V^T of 16 columns and a block's 32 tokens, in the order of the second product (see above).  A wave's block of V
-// lies in LDS as rows of DP; the 16-byte pieces of a row change places by its number, so that the rows that
-// are read together lie in different banks.
-template <int DP>
-__device__ inline int v_piece(int row, int piece) { return piece ^ (2 * (row & 7) & (DP / 8 - 1)); }
-
+// V^T of 16 columns and a block's 32 tokens, in the order of the second product (see above).
 template <int DP>
 __device__ inline u32x4 v_tile(const uint16_t *s_v, int d)
 {
-    typedef __attribute__((ext_vector_type(4))) short s16x4;
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const int col = threadIdx.x & 15, grp = (threadIdx.x & 63) >> 4;
     u32x2 v[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int row = h * 16 + grp * 4 + (col >> 2);
-        const uint16_t *at = s_v + row * DP + v_piece<DP>(row, 2 * d + ((col >> 1) & 1)) * 8 + (col & 1) * 4;
-        v[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at));
+        v[h] = read_transposed(s_v + row * DP + swizzled<DP>(row, 2 * d + ((col >> 1) & 1)) * 8 + (col & 1) * 4);
     }
     return u32x4{v[0][0], v[0][1], v[1][0], v[1][1]};
-}
-
-__device__ inline bool not_finite(u32x4 v)       // any of eight bf16
-{
-    bool r = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r |= (v[i] & 0x7F800000u) == 0x7F800000u || (v[i] & 0x7F80u) == 0x7F80u;
-    return r;
 }
 
 // DP: width of a head rounded up to what the products take; loads beyond the head's own width give zeros.
@@ -170,20 +136,17 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttnParams p)
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, grp = lane >> 4;
-    const int chunk = p.plan[0], items = min(p.plan[1 + p.b.n_seqs], p.max_items);
+    const Plan plan = plan_of<kRows>(p);
+    const int chunk = plan.chunk;
     const int D = p.c.dim;
     uint16_t *s_v = reinterpret_cast<uint16_t *>(s_mem) + wave * kBlock * DP;
     float *s_o = reinterpret_cast<float *>(s_mem);
 
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        const int s = wave_find(p.plan + 1, p.b.n_seqs, item);
-        const Seq q = seq_of(p.b, s);
-        int left = item - p.plan[1 + s];
-        const int head = left % p.c.n_heads;
-        left /= p.c.n_heads;
-        const int cuts = splits_of(reach_of(p, q), chunk);
-        const int tile = left / cuts, cut = left - tile * cuts;
-        const Range rg = range_of(p, q, tile, chunk);
+    for (int n = blockIdx.x; n < plan.items; n += gridDim.x) {
+        Seq q;
+        const Item it = item_of<kRows>(p, plan, n, q);
+        const int s = it.s, head = it.head, tile = it.tile, cut = it.cut;
+        const Range rg = range_of<kRows>(p, q, tile, chunk);
         if (cut >= rg.splits) continue;
         const int lo = rg.lo + cut * chunk, hi = min(rg.hi, lo + chunk);
 
@@ -241,7 +204,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttnParams p)
 #pragma unroll
             for (int n = 0; n < VL; ++n) {
                 const int row = n * RPL + lane / CH;
-                *reinterpret_cast<u32x4 *>(s_v + row * DP + v_piece<DP>(row, lane % CH) * 8) = vx[n];
+                *reinterpret_cast<u32x4 *>(s_v + row * DP + swizzled<DP>(row, lane % CH) * 8) = vx[n];
             }
             f32x4 sc[2];
 #pragma unroll
@@ -297,21 +260,19 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttnParams p)
                     o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v_tile<DP>(s_v, d)), pf, o[d] * shrink, 0, 0, 0);
             } else {
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] *= shrink;
+                for (int d = 0; d < DT; ++d)
+                    o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(finite_part(as_bf16x8(v_tile<DP>(s_v, d))), pf, o[d] * shrink, 0, 0, 0);
+                // the rest reaches the rows that see it: whatever the weight, infinity or NaN stays what it is
 #pragma unroll 1
-                for (int row = 0; row < kRows; ++row) {       // one row at a time, with zeros for what it does not see
-                    const int row_lo = __shfl(see_lo, row), row_hi = __shfl(see_hi, row);
+                for (int j = 0; j < kBlock; ++j) {
+                    if (j0 + j < see_lo || j0 + j >= see_hi) continue;
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        bf16x8 v8 = as_bf16x8(v_tile<DP>(s_v, d));
+                    for (int d = 0; d < DT; ++d)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int j = j0 + (e >> 2) * 16 + grp * 4 + (e & 3);
-                            if (j < row_lo || j >= row_hi) v8[e] = (__bf16)0.f;
+                        for (int e = 0; e < 4; ++e) {
+                            const int c = d * 16 + grp * 4 + e;
+                            o[d][e] += odd_part(s_v[j * DP + swizzled<DP>(j, c >> 3) * 8 + (c & 7)]);
                         }
-                        const f32x4 with = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, pf, o[d], 0, 0, 0);
-                        if (col == row) o[d] = with;
-                    }
                 }
             }
             __builtin_amdgcn_wave_barrier();
@@ -355,13 +316,13 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttnParams p)
                     b[1] = pack_bf16_rne(sum[2], sum[3]);
                     *reinterpret_cast<u32x2 *>(p.out + rt * p.ldo + (int64_t)rh * D + d) = b;
                 } else {
-                    st16f(p.part_o + ((int64_t)item * kRows + row) * D + d, sum);
+                    st16f(p.part_o + ((int64_t)it.slot * kRows + row) * D + d, sum);
                 }
             }
             if ((threadIdx.x & 15) == 0) {
                 if (!whole) {
-                    p.part_ml[((int64_t)item * kRows + row) * 2] = top;
-                    p.part_ml[((int64_t)item * kRows + row) * 2 + 1] = total;
+                    p.part_ml[((int64_t)it.slot * kRows + row) * 2] = top;
+                    p.part_ml[((int64_t)it.slot * kRows + row) * 2 + 1] = total;
                 } else if (p.lse) {
                     p.lse[rt * p.heads + rh] = total == 0.f ? -INFINITY : (ref * p.scale_log2 + __builtin_amdgcn_logf(total)) * kLn2;
                 }
@@ -371,6 +332,26 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttnParams p)
     }
 }
 
+// Where the partial results of a row lie, -1 if its range was not cut.
+struct Parts {
+    int64_t first;
+    int cuts;
+};
+
+template <int R>
+__device__ inline Parts parts_of(const AttnParams &p, const Seq &q, int s, int r, int head)
+{
+    const Plan plan = plan_of<R>(p);
+    const int tile = r / R;
+    Parts x = {-1, range_of<R>(p, q, tile, plan.chunk).splits};
+    if (x.cuts > 1) {
+        const int cuts = splits_of(reach_of<R>(p, q), plan.chunk);
+        const int slot = plan.slot[s] + tile * cuts * p.c.n_heads + head;
+        x.first = (int64_t)slot * R + r - tile * R;
+    }
+    return x;
+}
+
 // Joins the cuts of rows whose range was cut: a wave per row and head, by the rule of the running softmax.
 __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
 {
@@ -378,27 +359,28 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
     const int n = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     if (n >= p.b.n_rows * p.heads) return;
     const int t = n / p.heads, qh = n - t * p.heads;
-    const int chunk = p.plan[0];
     const int s = wave_find(p.b.row_start, p.b.n_seqs, t);
     const Seq q = seq_of(p.b, s);
     const int head = qh / p.group;
-    const int r = (t - p.b.row_start[s]) * p.group + qh - head * p.group;
-    const int tile = r / kRows, row = r - tile * kRows;
-    const Range rg = range_of(p, q, tile, chunk);
-    if (rg.splits == 1) return;
-    const int cuts = splits_of(reach_of(p, q), chunk);
-    const int64_t first = p.plan[1 + s] + ((int64_t)tile * cuts) * p.c.n_heads + head;
+    const int i = t - p.b.row_start[s];
+    if (i < 0 || i >= q.rows) return;
+    const int r = i * p.group + qh - head * p.group;
+    const bool is_short = q.rows * p.group <= p.short_limit;
+    const Parts parts = is_short ? parts_of<kShortTile>(p, q, s, r, head) : parts_of<kLongTile>(p, q, s, r, head);
+    if (parts.first < 0) return;
+    const float *ml = is_short ? p.part_ml : p.long_ml, *po = is_short ? p.part_o : p.long_o;
+    const int64_t step = (int64_t)p.c.n_heads * (is_short ? kShortTile : kLongTile);
     float m = -INFINITY;
-    for (int c = 0; c < rg.splits; ++c) m = fmaxf(m, p.part_ml[((first + c * p.c.n_heads) * kRows + row) * 2]);
+    for (int c = 0; c < parts.cuts; ++c) m = fmaxf(m, ml[(parts.first + c * step) * 2]);
     const float ref = m == -INFINITY ? 0.f : m;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     float total = 0.f;
     const int d = lane * 4;
-    for (int c = 0; c < rg.splits; ++c) {
-        const int64_t at = (first + c * p.c.n_heads) * kRows + row;
-        const float f = __builtin_amdgcn_exp2f((p.part_ml[at * 2] - ref) * p.scale_log2);
-        total += f * p.part_ml[at * 2 + 1];
-        if (d < p.c.dim) sum += ld16f(p.part_o + at * p.c.dim + d) * f;
+    for (int c = 0; c < parts.cuts; ++c) {
+        const int64_t at = parts.first + c * step;
+        const float f = __builtin_amdgcn_exp2f((ml[at * 2] - ref) * p.scale_log2);
+        total += f * ml[at * 2 + 1];
+        if (d < p.c.dim) sum += ld16f(po + at * p.c.dim + d) * f;
     }
     const float norm = total == 0.f ? 0.f : 1.f / total;
     if (d < p.c.dim) {
@@ -412,38 +394,73 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Upper bounds from what the host knows.
-int64_t max_items_of(int n_seqs, int n_rows, int heads, int kv_heads)
+// Which kernels a batch takes, and upper bounds of their work items, from what the host knows.
+struct Kinds {
+    bool has_short, has_long;
+    int limit;                            // rows x group of a sequence that goes in short tiles
+    int64_t short_items, long_items;
+};
+
+Kinds kinds_of(int n_seqs, int n_rows, int max_rows, int heads, int kv_heads)
 {
     const int64_t group = heads / kv_heads;
-    const int64_t tiles = std::min<int64_t>(n_seqs, n_rows) + (int64_t)n_rows * group / kRows;
-    return kTargetItems + tiles * kv_heads;
+    const int64_t most = max_rows > 0 ? std::min(max_rows, n_rows) : n_rows;
+    Kinds k;
+    k.has_long = most * group > kShortLimit;
+    k.has_short = !k.has_long || !(max_rows > 0 && (int64_t)max_rows * n_seqs == n_rows);
+    // a sequence with more rows than the host thought still has to go somewhere
+    k.limit = !k.has_long ? INT_MAX : !k.has_short ? 0 : kShortLimit;
+    const int64_t some = std::min(n_seqs, n_rows);
+    k.short_items = kShortTarget + kv_heads * (some + n_rows * group / kShortTile);
+    k.long_items = kLongTarget + kv_heads * (some + n_rows * group / kLongTile);
+    return k;
+}
+
+struct Ws {
+    size_t plan, short_ml, short_o, long_ml, long_o, bytes;
+};
+
+Ws ws_of(int n_seqs, const Kinds &k, int dim)
+{
+    Ws w;
+    w.plan = 0;
+    w.short_ml = up256((kPlanHead + 4 * (size_t)n_seqs) * 4);
+    w.short_o = w.short_ml + up256(k.has_short ? 2 * (size_t)kShortTarget * kShortTile * 8 : 0);
+    w.long_ml = w.short_o + up256(k.has_short ? 2 * (size_t)kShortTarget * kShortTile * dim * 4 : 0);
+    w.long_o = w.long_ml + up256(k.has_long ? 2 * (size_t)kLongTarget * kLongTile * 8 : 0);
+    w.bytes = w.long_o + up256(k.has_long ? 2 * (size_t)kLongTarget * kLongTile * dim * 4 : 0);
+    return w;
 }
 
 }  // namespace
 
 size_t attention_ws_bytes(int n_seqs, int n_rows, int max_rows, int heads, int kv_heads, int dim)
 {
-    (void)max_rows;
-    const int64_t items = max_items_of(n_seqs, n_rows, heads, kv_heads);
-    return up256((size_t)(n_seqs + 2) * 4) + up256((size_t)items * kRows * 8) + (size_t)items * kRows * dim * 4;
+    return ws_of(n_seqs, kinds_of(n_seqs, n_rows, max_rows, heads, kv_heads), dim).bytes;
 }
 
 hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s)
 {
-    (void)max_rows;
-    p.max_items = (int)max_items_of(p.b.n_seqs, p.b.n_rows, p.heads, p.c.n_heads);
+    const Kinds k = kinds_of(p.b.n_seqs, p.b.n_rows, max_rows, p.heads, p.c.n_heads);
+    const Ws at = ws_of(p.b.n_seqs, k, p.c.dim);
     char *w = static_cast<char *>(ws);
-    p.plan = reinterpret_cast<int32_t *>(w);
-    w += up256((size_t)(p.b.n_seqs + 2) * 4);
-    p.part_ml = reinterpret_cast<float *>(w);
-    w += up256((size_t)p.max_items * kRows * 8);
-    p.part_o = reinterpret_cast<float *>(w);
+    p.plan = reinterpret_cast<int32_t *>(w + at.plan);
+    p.part_ml = reinterpret_cast<float *>(w + at.short_ml);
+    p.part_o = reinterpret_cast<float *>(w + at.short_o);
+    p.long_ml = reinterpret_cast<float *>(w + at.long_ml);
+    p.long_o = reinterpret_cast<float *>(w + at.long_o);
+    p.short_limit = k.limit;
     hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
-    const dim3 grid(std::min(p.max_items, 1024)), block(kWaves * 64);
-    if (p.c.dim <= 64) hipLaunchKernelGGL(attend_kernel<64>, grid, block, 0, s, p);
-    else if (p.c.dim <= 128) hipLaunchKernelGGL(attend_kernel<128>, grid, block, 0, s, p);
-    else hipLaunchKernelGGL(attend_kernel<256>, grid, block, 0, s, p);
+    if (k.has_long) {
+        const hipError_t e = launch_attend_long(p, (int)std::min<int64_t>(k.long_items, INT_MAX), s);
+        if (e != hipSuccess) return e;
+    }
+    if (k.has_short) {
+        const dim3 grid((unsigned)std::min<int64_t>(k.short_items, 1024)), block(kWaves * 64);
+        if (p.c.dim <= 64) hipLaunchKernelGGL(attend_kernel<64>, grid, block, 0, s, p);
+        else if (p.c.dim <= 128) hipLaunchKernelGGL(attend_kernel<128>, grid, block, 0, s, p);
+        else hipLaunchKernelGGL(attend_kernel<256>, grid, block, 0, s, p);
+    }
     const int64_t waves = (int64_t)p.b.n_rows * p.heads;
     hipLaunchKernelGGL(join_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, p);
     return hipGetLastError();

@@ -49,10 +49,10 @@ struct AttnParams {
     int64_t ldq, ldo;
     float scale_log2;             // scale / ln 2
     int heads, group, causal, window;
-    FastDiv group_div;
-    int32_t *plan;                // device: see kv_attention.hip
-    float *part_o, *part_ml;
-    int max_items;
+    int short_limit;              // rows x group of a sequence up to which it goes in short tiles
+    int32_t *plan;                // device: see kv_attention.h
+    float *part_o, *part_ml;      // partial results of short tiles whose range is cut: sums, and maximum and sum of weights
+    float *long_o, *long_ml;
 };
 
 struct PlanParams {
