@@ -71,9 +71,9 @@ __device__ inline int reach_of(const AttnParams &p, const Seq &q)
 
 __device__ inline int splits_of(int reach, int chunk) { return reach <= chunk ? 1 : (reach + chunk - 1) / chunk; }
 
-// A tile's tokens [lo, hi) and the number of its cuts that are not empty.
+// A tile's tokens [lo, hi), into how many items they are cut, and the tokens of each.
 struct Range {
-    int lo, hi, splits;
+    int lo, hi, splits, each;
 };
 
 template <int R>
@@ -85,6 +85,8 @@ __device__ inline Range range_of(const AttnParams &p, const Seq &q, int tile, in
     r.lo = p.window ? max(0, q.pos0 + i0 - p.window + 1) : 0;
     if (r.lo >= r.hi) r.lo = r.hi = 0;
     r.splits = splits_of(r.hi - r.lo, chunk);
+    // evenly, in multiples of 64, as the chunk is one: no cut is empty, as splits - 1 chunks are not enough
+    r.each = r.splits == 1 ? r.hi - r.lo : ((r.hi - r.lo + r.splits - 1) / r.splits + 63) >> 6 << 6;
     return r;
 }
 

@@ -137,7 +137,6 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttnParams p)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, grp = lane >> 4;
     const Plan plan = plan_of<kRows>(p);
-    const int chunk = plan.chunk;
     const int D = p.c.dim;
     uint16_t *s_v = reinterpret_cast<uint16_t *>(s_mem) + wave * kBlock * DP;
     float *s_o = reinterpret_cast<float *>(s_mem);
@@ -146,9 +145,9 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttnParams p)
         Seq q;
         const Item it = item_of<kRows>(p, plan, n, q);
         const int s = it.s, head = it.head, tile = it.tile, cut = it.cut;
-        const Range rg = range_of<kRows>(p, q, tile, chunk);
+        const Range rg = range_of<kRows>(p, q, tile, plan.chunk);
         if (cut >= rg.splits) continue;
-        const int lo = rg.lo + cut * chunk, hi = min(rg.hi, lo + chunk);
+        const int lo = rg.lo + cut * rg.each, hi = min(rg.hi, lo + rg.each);
 
         // this lane's row
         const int r = tile * kRows + col;

@@ -5,12 +5,14 @@
 // of the tile, its two lane halves hold different tokens, and P goes from the first product's result to the second
 // one's operand without leaving its lane (16 tokens: 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 for lane half h).
 //
-// The running maximum only moves when a score passes it by more than 2^8 in weight, so most steps rescale nothing;
-// the weights stay below 2^8 and the sums are the same up to rounding.
+// Weights need not be taken against the running maximum, only against a value near it: the reference is the maximum of the
+// first tokens that a row sees, and moves to the running one when the weights of a step pass 2^10.  So most steps look for
+// no maximum and rescale nothing; the sums are the same up to rounding.
 #include <limits.h>
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "kv_attention.h"
 
@@ -21,33 +23,40 @@ namespace {
 constexpr int kRows = kLongTile;
 constexpr int kTokens = 64;              // of a step
 constexpr int kWaves = 4;
-constexpr float kSlack = 8.f;            // the maximum's, in powers of two
+constexpr float kMost = 1024.f;          // sum of a lane's 32 weights up to which the reference stays
 constexpr float kExact = 4096.f;         // scaled maxima up to which e^(s - m) is formed with one rounding of m
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 __device__ __align__(16) const unsigned zeros[4] = {0u, 0u, 0u, 0u};
 
-// V^T of 32 columns and 16 tokens.
+typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) const uint16_t lds_u16;
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+__device__ inline float other_half(float x) { return __shfl_xor(x, 32); }
+
+// The value of the lane of the same DP / 8 lanes that holds load j's row.
 template <int DP>
-__device__ inline bf16x8 v_tile(const uint16_t *s_v, int tokens, int d)
+__device__ inline int of_load(int x, int j)
 {
-    const int l = threadIdx.x & 15, grp = (threadIdx.x & 63) >> 4;
-    u32x2 v[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int row = tokens + j * 8 + (grp >> 1) * 4 + (l >> 2);
-        v[j] = read_transposed(s_v + row * DP + swizzled<DP>(row, d * 4 + (grp & 1) * 2 + ((l >> 1) & 1)) * 8 + (l & 1) * 4);
+    if (DP == 64) return __shfl(x, (threadIdx.x & 56) + j);
+    switch (j) {                          // row_newbcast: one lane of each 16
+    case 0: return __builtin_amdgcn_update_dpp(0, x, 0x150, 0xf, 0xf, true);
+    case 1: return __builtin_amdgcn_update_dpp(0, x, 0x151, 0xf, 0xf, true);
+    case 2: return __builtin_amdgcn_update_dpp(0, x, 0x152, 0xf, 0xf, true);
+    case 3: return __builtin_amdgcn_update_dpp(0, x, 0x153, 0xf, 0xf, true);
+    case 4: return __builtin_amdgcn_update_dpp(0, x, 0x154, 0xf, 0xf, true);
+    case 5: return __builtin_amdgcn_update_dpp(0, x, 0x155, 0xf, 0xf, true);
+    case 6: return __builtin_amdgcn_update_dpp(0, x, 0x156, 0xf, 0xf, true);
+    default: return __builtin_amdgcn_update_dpp(0, x, 0x157, 0xf, 0xf, true);
     }
-    return as_bf16x8(u32x4{v[0][0], v[0][1], v[1][0], v[1][1]});
 }
 
-__device__ inline float other_half(float x)
-{
-    return __shfl_xor(x, 32);
-}
-
-template <int DP>
+// DP: width of a head rounded up.  FULL: it is the width itself; otherwise pieces beyond it are filled with zeros.
+template <int DP, bool FULL>
 __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_kernel(AttnParams p)
 {
     constexpr int KS = DP / 16;          // steps of the first product
@@ -55,21 +64,22 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     constexpr int CH = DP / 8;           // 16-byte pieces of a row
     constexpr int RPL = 64 / CH;         // rows that a wave's load covers
     constexpr int NL = kTokens / RPL / kWaves;           // loads of K and of V per wave and step
-    constexpr int STAGE = kTokens * DP;  // elements of K or V in LDS
-    __shared__ __align__(16) uint16_t s_kv[2][2][STAGE];
+    constexpr int ROW = DP * 2;          // bytes
+    constexpr int STAGE = kTokens * ROW; // of K or V in LDS
+    __shared__ __align__(16) unsigned char s_kv[2][2][STAGE];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
-    const int D = p.c.dim;
+    const int D = FULL ? DP : p.c.dim;
     const Plan plan = plan_of<kRows>(p);
     const int n = blockIdx.x;
     if (n >= plan.items) return;
     Seq q;
     const Item it = item_of<kRows>(p, plan, n, q);
-    const int tile = (it.cuts > 1 ? it.tile : tiles_of<kRows>(p, q) - 1 - it.tile);      // long ranges first
+    const int tile = it.cuts > 1 ? it.tile : tiles_of<kRows>(p, q) - 1 - it.tile;        // long ranges first
     const Range rg = range_of<kRows>(p, q, tile, plan.chunk);
     if (it.cut >= rg.splits) return;
-    const int lo = rg.lo + it.cut * plan.chunk, hi = min(rg.hi, lo + plan.chunk);
+    const int lo = rg.lo + it.cut * rg.each, hi = min(rg.hi, lo + rg.each);
 
     // this lane's row, and the tokens that it, some row and every row of its wave see
     const int r0 = tile * kRows + wave * 32;
@@ -98,58 +108,66 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     f32x16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = f32x16{};
-    float m = -INFINITY, ms = -INFINITY, l = 0.f;      // maximum, the same in powers of two, this lane's part of the sum
+    // The reference m that weights are taken against (of a row that has seen nothing: none), the same in powers of two,
+    // and this lane's part of the sum.  A row beyond the tile's takes zero, so that it never asks for another.
+    float m = real ? -INFINITY : 0.f, ms = m, l = 0.f;
+    bool big = false;
 
-    // this wave's loads: rows (wave * NL + j) * RPL + lane / CH of a step, the piece that belongs at place lane % CH
+    // LDS addresses of the operands: only constants are added to them in the loop
+    lds_byte *const lds0 = (lds_byte *)&s_kv[0][0][0];
+    lds_byte *k_at[KS], *v_at[DT];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) k_at[ks] = lds0 + col * ROW + swizzled<DP>(col, ks * 2 + half) * 16;
+    {
+        const int l16 = lane & 15, grp = lane >> 4, row = (grp >> 1) * 4 + (l16 >> 2);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+            v_at[d] = lds0 + STAGE + row * ROW + swizzled<DP>(row, d * 4 + (grp & 1) * 2 + (l16 >> 1 & 1)) * 16 + (l16 & 1) * 8;
+    }
+
+    // This wave's loads of a step: load j covers rows (wave * NL + j) * RPL + lane / CH.  Lane j of every CH lanes looks up
+    // the page of load j's row and hands the place to the others; a lane fetches the piece that belongs at its place.
     const int32_t *table = p.b.table + (int64_t)it.s * p.b.max_pages;
     const int place_mask = (1 << p.c.page_shift) - 1;
-    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)&s_kv[0][0][0];
     const uint16_t *kbase = p.c.k + it.head * p.c.head_stride, *vbase = p.c.v + it.head * p.c.head_stride;
-    int page[NL];
-    const auto token_of = [&](int j0, int j) { return min(j0 + (wave * NL + j) * RPL + lane / CH, hi - 1); };
-    const auto fetch_pages = [&](int j0) {
+    const int my_row = (wave * NL + (lane & (NL - 1))) * RPL + lane / CH;
+    int piece[2];                         // of even and of odd loads
 #pragma unroll
-        for (int j = 0; j < NL; ++j) page[j] = table[token_of(j0, j) >> p.c.page_shift];
-    };
+    for (int j = 0; j < 2; ++j) piece[j] = swizzled<DP>((wave * NL + j) * RPL + lane / CH, lane % CH) * 8;
+    static_assert(RPL * 2 >= 8 || DP > 128, "the swizzle repeats after two loads");
+    int page = 0;
+    unsigned bad = 0;
+    const auto fetch_page = [&](int j0) { page = table[min(j0 + my_row, hi - 1) >> p.c.page_shift]; };
     const auto fetch = [&](int j0, int stage) {
+        bad |= (unsigned)page >= (unsigned)p.c.n_pages;
+        const int64_t at = (int64_t)min((unsigned)page, (unsigned)p.c.n_pages - 1u) * p.c.page_stride +
+                           (int64_t)(min(j0 + my_row, hi - 1) & place_mask) * p.c.token_stride;
+        const int at_lo = (int)at, at_hi = (int)(at >> 32);
 #pragma unroll
         for (int j = 0; j < NL; ++j) {
-            const int row = (wave * NL + j) * RPL + lane / CH;
-            const int token = token_of(j0, j);
-            const int piece = swizzled<DP>(row, lane % CH);
-            const int64_t at = checked_page(page[j], p.c.n_pages, p.b.status) * p.c.page_stride +
-                               (int64_t)(token & place_mask) * p.c.token_stride + piece * 8;
-            const bool in = piece * 8 < D;
-            const unsigned to = lds0 + ((stage * 2) * STAGE + (wave * NL + j) * RPL * DP) * 2;
-            load_to_lds<false>(in ? (const void *)(kbase + at) : (const void *)zeros, to);
-            load_to_lds<false>(in ? (const void *)(vbase + at) : (const void *)zeros, to + STAGE * 2);
+            const int64_t row = (int64_t)(((uint64_t)(unsigned)of_load<DP>(at_hi, j) << 32) | (unsigned)of_load<DP>(at_lo, j));
+            const int pc = DP > 128 ? swizzled<DP>((wave * NL + j) * RPL + lane / CH, lane % CH) * 8 : piece[j & 1];
+            const bool in = FULL || pc < D;
+            const unsigned to = (unsigned)(uintptr_t)lds0 + stage * 2 * STAGE + (wave * NL + j) * 1024;
+            load_to_lds<false>(in ? (const void *)(kbase + row + pc) : (const void *)zeros, to);
+            load_to_lds<false>(in ? (const void *)(vbase + row + pc) : (const void *)zeros, to + STAGE);
         }
     };
-    if (lo < hi) {
-        fetch_pages(lo);
-        fetch(lo, 0);
-        fetch_pages(min(lo + kTokens, hi - 1));
-    }
-    int stage = 0;
-    for (int j0 = lo; j0 < hi; j0 += kTokens, stage ^= 1) {
-        wait_loads<0>();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        if (j0 + kTokens < hi) {
-            fetch(j0 + kTokens, stage ^ 1);
-            fetch_pages(min(j0 + 2 * kTokens, hi - 1));
-        }
-        if (j0 >= any_hi || j0 + kTokens <= any_lo) continue;
-        const uint16_t *s_k = s_kv[stage][0], *s_v = s_kv[stage][1];
+
+    // 64 tokens from j0 on, in LDS at `stage`
+    const auto step = [&](int j0, auto stage_c) {
+        constexpr int AT = decltype(stage_c)::value * 2 * STAGE;
+        const auto v_tile = [&](int k, int d) {
+            const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v_at[d] + (AT + k * 16 * ROW))));
+            const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(v_at[d] + (AT + k * 16 * ROW + 8 * ROW))));
+            return as_bf16x8(u32x4{a[0], a[1], b[0], b[1]});
+        };
         f32x16 s[2] = {f32x16{}, f32x16{}};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = h * 32 + col;
-                const u32x4 k = *reinterpret_cast<const u32x4 *>(s_k + row * DP + swizzled<DP>(row, ks * 2 + half) * 8);
-                s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k), qf[ks], s[h], 0, 0, 0);
-            }
+            for (int h = 0; h < 2; ++h)
+                s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(lds_u32x4 *)(k_at[ks] + (AT + h * 32 * ROW))), qf[ks], s[h], 0, 0, 0);
         const bool edge = j0 < all_lo || j0 + kTokens > all_hi;
         if (edge) {
 #pragma unroll
@@ -160,66 +178,75 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
                     if (j < see_lo || j >= see_hi) s[h][e] = -INFINITY;
                 }
         }
-        float top = s[0][0];
+        bf16x8 pf[4];
+        float sum;
+        const auto weigh = [&](float mul, float sub) {
+            sum = 0.f;
 #pragma unroll
-        for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
-        top = fmaxf(top, other_half(top));
-        const float tops = top * p.scale_log2;
-        if (__any(tops > ms + kSlack)) {
-            const float now = fmaxf(m, top), now_s = fmaxf(ms, tops);
-            const float f = fabsf(now_s) <= kExact ? __builtin_amdgcn_exp2f(ms - now_s)
-                                                  : __builtin_amdgcn_exp2f((m - (now == -INFINITY ? 0.f : now)) * p.scale_log2);
-            const float keep = now == -INFINITY ? 1.f : f;
+            for (int k = 0; k < 4; ++k) {
+                u32x4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][(k & 1) * 8 + 2 * e], mul, -sub));
+                    const float b = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][(k & 1) * 8 + 2 * e + 1], mul, -sub));
+                    sum += a + b;
+                    w[e] = pack_bf16_rne(a, b);
+                }
+                pf[k] = as_bf16x8(w);
+            }
+        };
+        bool again = big;
+        if (!big) {
+            weigh(p.scale_log2, ms == -INFINITY ? 0.f : ms);
+            again = __any(sum > kMost || ms == -INFINITY);
+        }
+        if (again) {
+            float top = s[0][0];
+#pragma unroll
+            for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
+            top = fmaxf(top, other_half(top));
+            const float now = fmaxf(m, top), now_s = fmaxf(ms, top * p.scale_log2);
+            const bool was_big = big;
+            big = __any(fabsf(now_s) > kExact && now > -INFINITY);
+            const float ref = now == -INFINITY ? 0.f : now;
+            // scores so large that m's own rounding in powers of two would show are subtracted before they are scaled
+            const float keep = now == -INFINITY ? 1.f
+                               : was_big || big ? __builtin_amdgcn_exp2f((m - ref) * p.scale_log2)
+                                                : __builtin_amdgcn_exp2f(ms - now_s);
             l *= keep;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] *= keep;
             m = now;
             ms = now_s;
-        }
-        float mul = p.scale_log2, sub = ms == -INFINITY ? 0.f : ms;
-        if (__any(fabsf(sub) > kExact)) {         // scores so large that their scaled difference has to be exact
-            const float ref = m == -INFINITY ? 0.f : m;
+            if (big) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) s[e >> 4][e & 15] = (s[e >> 4][e & 15] - ref) * p.scale_log2;
-            mul = 1.f;
-            sub = 0.f;
-        }
-        bf16x8 pf[4];
-        float sum = 0.f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            u32x4 w;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float a = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][(k & 1) * 8 + 2 * e], mul, -sub));
-                const float b = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][(k & 1) * 8 + 2 * e + 1], mul, -sub));
-                sum += a + b;
-                w[e] = pack_bf16_rne(a, b);
+                for (int e = 0; e < 32; ++e) s[e >> 4][e & 15] = (s[e >> 4][e & 15] - ref) * p.scale_log2;
+                weigh(1.f, 0.f);
+            } else {
+                weigh(p.scale_log2, now_s == -INFINITY ? 0.f : now_s);
             }
-            pf[k] = as_bf16x8(w);
         }
         l += sum;
         // V of a token that some rows must not see may be no number: 0 * NaN would reach them
         bool odd = false;
         if (edge) {
-#pragma unroll 1
+#pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int d = 0; d < DT; ++d) odd |= not_finite(__builtin_bit_cast(u32x4, v_tile<DP>(s_v, k * 16, d)));
+                for (int d = 0; d < DT; ++d) odd |= not_finite(__builtin_bit_cast(u32x4, v_tile(k, d)));
             odd = __any(odd);
         }
         if (!odd) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_tile<DP>(s_v, k * 16, d), pf[k], o[d], 0, 0, 0);
+                for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_tile(k, d), pf[k], o[d], 0, 0, 0);
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_part(v_tile<DP>(s_v, k * 16, d)), pf[k], o[d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_part(v_tile(k, d)), pf[k], o[d], 0, 0, 0);
             // the rest reaches the rows that see it: whatever the weight, infinity or NaN stays what it is
 #pragma unroll 1
             for (int j = 0; j < kTokens; ++j) {
@@ -229,11 +256,35 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int c = d * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-                        o[d][e] += odd_part(s_v[j * DP + swizzled<DP>(j, c >> 3) * 8 + (c & 7)]);
+                        o[d][e] += odd_part(*(lds_u16 *)(lds0 + AT + STAGE + j * ROW + swizzled<DP>(j, c >> 3) * 16 + (c & 7) * 2));
                     }
             }
         }
+    };
+    // the stage is full, and every wave has read what the next fetch overwrites
+    const auto meet = [&] {
+        wait_loads<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+    };
+    const auto turn = [&](int j0, auto stage_c) {
+        meet();
+        if (j0 + kTokens < hi) {
+            fetch(j0 + kTokens, decltype(stage_c)::value ^ 1);
+            fetch_page(j0 + 2 * kTokens);
+        }
+        if (j0 < any_hi && j0 + kTokens > any_lo) step(j0, stage_c);
+    };
+    if (lo < hi) {
+        fetch_page(lo);
+        fetch(lo, 0);
+        fetch_page(lo + kTokens);
     }
+    for (int j0 = lo; j0 < hi; j0 += 2 * kTokens) {
+        turn(j0, std::integral_constant<int, 0>{});
+        if (j0 + kTokens < hi) turn(j0 + kTokens, std::integral_constant<int, 1>{});
+    }
+    if (bad) atomicOr(p.b.status, LORA_STATUS_BAD_PAGE);
     l += other_half(l);
     if (!real) return;
     const float ref = ms == -INFINITY ? 0.f : ms;
@@ -273,9 +324,17 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
 hipError_t launch_attend_long(const AttnParams &p, int max_items, hipStream_t s)
 {
     const dim3 grid(max_items), block(kWaves * 64);
-    if (p.c.dim <= 64) hipLaunchKernelGGL(attend_long_kernel<64>, grid, block, 0, s, p);
-    else if (p.c.dim <= 128) hipLaunchKernelGGL(attend_long_kernel<128>, grid, block, 0, s, p);
-    else hipLaunchKernelGGL(attend_long_kernel<256>, grid, block, 0, s, p);
+#define LORA_LONG(DP)                                                                                       \
+    if (p.c.dim == DP) hipLaunchKernelGGL((attend_long_kernel<DP, true>), grid, block, 0, s, p);            \
+    else if (p.c.dim < DP) hipLaunchKernelGGL((attend_long_kernel<DP, false>), grid, block, 0, s, p);
+    if (p.c.dim <= 64) {
+        LORA_LONG(64)
+    } else if (p.c.dim <= 128) {
+        LORA_LONG(128)
+    } else {
+        LORA_LONG(256)
+    }
+#undef LORA_LONG
     return hipGetLastError();
 }
 
