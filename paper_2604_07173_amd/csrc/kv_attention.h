@@ -16,26 +16,13 @@ constexpr int kShortMinSplit = 256, kLongMinSplit = 512;   // tokens of a cut ra
 constexpr int kShortLimit = 64;          // rows x group up to which a sequence goes in short tiles
 constexpr float kLn2 = 0.6931471805599453f;
 
-// The device plan: a head of kPlanHead words, then four arrays over the sequences.
-enum { kChunkShort, kChunkLong, kItemsShort, kItemsLong, kPlanHead = 16 };
+constexpr int kInlineSeqs = 256;         // sequences up to which every workgroup makes the plan for itself, in LDS: one launch less
 
-struct Plan {
-    const int32_t *head, *base, *slot;   // work items and partial results before each sequence
-    int chunk, items;
-};
-
-template <int R>
-__device__ inline Plan plan_of(const AttnParams &p)
-{
-    constexpr bool SHORT = R == kShortTile;
-    Plan q;
-    q.head = p.plan;
-    q.base = p.plan + kPlanHead + (SHORT ? 0 : 2) * p.b.n_seqs;
-    q.slot = q.base + p.b.n_seqs;
-    q.chunk = p.plan[SHORT ? kChunkShort : kChunkLong];
-    q.items = p.plan[SHORT ? kItemsShort : kItemsLong];
-    return q;
-}
+// The plan: a head of kPlanHead words, then kPlanArrays arrays over the sequences: work items and partial results before
+// each sequence, of short and of long tiles, and rows x heads to join.
+enum { kChunkShort, kChunkLong, kItemsShort, kItemsLong, kJoinUnits, kPlanHead = 8 };
+enum { kBaseShort, kSlotShort, kBaseLong, kSlotLong, kBaseJoin, kPlanArrays };
+constexpr int kInlineWords = kPlanHead + kPlanArrays * kInlineSeqs;
 
 struct Seq {
     int rows, len, pos0;                 // new rows, length, position of the first new row
@@ -90,22 +77,117 @@ __device__ inline Range range_of(const AttnParams &p, const Seq &q, int tile, in
     return r;
 }
 
+// Makes the plan with a workgroup of THREADS, into LDS or the workspace: cuts the ranges so that all work items of a kind
+// take about as long.  Rows that are no partition of the batch's give no work at all.
+template <int THREADS>
+__device__ inline void make_plan(const AttnParams &p, int32_t *plan, bool report)
+{
+    constexpr int WAVES = THREADS / 64;
+    __shared__ int64_t s_work[2][WAVES];
+    __shared__ int s_sum[kPlanArrays][WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = p.b.n_seqs;
+    int64_t work[2] = {0, 0};
+    unsigned bad = 0;
+    for (int s = tid; s < n; s += THREADS) {
+        const Seq q = seq_of(p.b, s);
+        if (p.b.seq_len[s] != q.len) bad |= 1;
+        const int first = p.b.row_start[s], end = p.b.row_start[s + 1];
+        if (first < 0 || end < first || end > p.b.n_rows || (s == 0 && first != 0) || (s == n - 1 && end != p.b.n_rows)) bad |= 2;
+        work[0] += (int64_t)tiles_of<kShortTile>(p, q) * reach_of<kShortTile>(p, q);
+        work[1] += (int64_t)tiles_of<kLongTile>(p, q) * reach_of<kLongTile>(p, q);
+    }
+    if (bad && report) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        work[0] += __shfl_xor(work[0], d);
+        work[1] += __shfl_xor(work[1], d);
+    }
+    if (lane == 0) s_work[0][wave] = work[0], s_work[1][wave] = work[1];
+    const bool no_rows = __syncthreads_or(bad & 2);
+    int chunk[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        int64_t all = 0;
+        for (int w = 0; w < WAVES; ++w) all += s_work[k][w];
+        const int64_t target = k ? kLongTarget : kShortTarget, least = k ? kLongMinSplit : kShortMinSplit;
+        const int64_t each = (all * p.c.n_heads + target - 1) / target;
+        chunk[k] = (int)min(((max(each, least) + 127) >> 7) << 7, (int64_t)1 << 30);
+    }
+    int base[kPlanArrays] = {};
+    for (int s0 = 0; s0 < n; s0 += THREADS) {
+        const int s = s0 + tid;
+        int own[kPlanArrays] = {}, v[kPlanArrays];
+        if (s < n && !no_rows) {
+            const Seq q = seq_of(p.b, s);
+            const int cut_s = splits_of(reach_of<kShortTile>(p, q), chunk[0]), cut_l = splits_of(reach_of<kLongTile>(p, q), chunk[1]);
+            const int tiles_s = tiles_of<kShortTile>(p, q), tiles_l = tiles_of<kLongTile>(p, q);
+            own[kBaseShort] = tiles_s * cut_s * p.c.n_heads;
+            own[kSlotShort] = cut_s > 1 ? own[kBaseShort] : 0;
+            own[kBaseLong] = tiles_l * cut_l * p.c.n_heads;
+            own[kSlotLong] = cut_l > 1 ? own[kBaseLong] : 0;
+            own[kBaseJoin] = (tiles_s ? cut_s : cut_l) > 1 ? q.rows * p.heads : 0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPlanArrays; ++k) v[k] = own[k];
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+            for (int k = 0; k < kPlanArrays; ++k) {
+                const int o = __shfl_up(v[k], d);
+                if (lane >= d) v[k] += o;
+            }
+        if (lane == 63)
+#pragma unroll
+            for (int k = 0; k < kPlanArrays; ++k) s_sum[k][wave] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPlanArrays; ++k) {
+            int total = 0;
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) v[k] += s_sum[k][w];
+                total += s_sum[k][w];
+            }
+            if (s < n) plan[kPlanHead + k * n + s] = base[k] + v[k] - own[k];
+            base[k] += total;
+        }
+    }
+    if (tid == 0) {
+        plan[kChunkShort] = chunk[0];
+        plan[kChunkLong] = chunk[1];
+        plan[kItemsShort] = base[kBaseShort];
+        plan[kItemsLong] = base[kBaseLong];
+        plan[kJoinUnits] = base[kBaseJoin];
+    }
+    __syncthreads();
+}
+
+// The plan of a workgroup of 256: made in s_plan, or what a launch before has left in the workspace.
+__device__ inline const int32_t *plan_of(const AttnParams &p, int32_t *s_plan)
+{
+    if (p.b.n_seqs > kInlineSeqs) return p.plan;
+    make_plan<256>(p, s_plan, blockIdx.x == 0);
+    return s_plan;
+}
+
 struct Item {
     int s, head, tile, cut, cuts, slot;
 };
 
 // Work item n: the cuts of a tile lie n_heads apart, tiles behind each other.
 template <int R>
-__device__ inline Item item_of(const AttnParams &p, const Plan &plan, int n, Seq &q)
+__device__ inline Item item_of(const AttnParams &p, const int32_t *plan, int n, Seq &q)
 {
+    const int32_t *base = plan + kPlanHead + (R == kShortTile ? kBaseShort : kBaseLong) * p.b.n_seqs;
     Item it;
-    it.s = wave_find(plan.base, p.b.n_seqs, n);
+    it.s = wave_find(base, p.b.n_seqs, n);
     q = seq_of(p.b, it.s);
-    const int left = n - plan.base[it.s];
-    it.slot = plan.slot[it.s] + left;
+    const int left = n - base[it.s];
+    it.slot = base[p.b.n_seqs + it.s] + left;
     const int pair = left / p.c.n_heads;
     it.head = left - pair * p.c.n_heads;
-    it.cuts = splits_of(reach_of<R>(p, q), plan.chunk);
+    it.cuts = splits_of(reach_of<R>(p, q), plan[R == kShortTile ? kChunkShort : kChunkLong]);
     it.tile = pair / it.cuts;
     it.cut = pair - it.tile * it.cuts;
     return it;

@@ -28,83 +28,8 @@ constexpr int kBlock = 32;               // tokens of a wave's step
 constexpr int kRows = kShortTile;
 constexpr int kPlanThreads = 1024;
 
-// Cuts the ranges so that all work items of a kind take about as long.
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
-{
-    constexpr int WAVES = kPlanThreads / 64;
-    __shared__ int64_t s_work[2][WAVES];
-    __shared__ int s_sum[4][WAVES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t work[2] = {0, 0};
-    unsigned bad = 0;
-    for (int s = threadIdx.x; s < p.b.n_seqs; s += kPlanThreads) {
-        const Seq q = seq_of(p.b, s);
-        if (p.b.seq_len[s] != q.len) bad |= 1;
-        const int first = p.b.row_start[s], end = p.b.row_start[s + 1];
-        if (first < 0 || end < first || end > p.b.n_rows || (s == 0 && first != 0) || (s == p.b.n_seqs - 1 && end != p.b.n_rows)) bad |= 2;
-        work[0] += (int64_t)tiles_of<kShortTile>(p, q) * reach_of<kShortTile>(p, q);
-        work[1] += (int64_t)tiles_of<kLongTile>(p, q) * reach_of<kLongTile>(p, q);
-    }
-    if (bad) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-#pragma unroll
-        for (int d = 32; d; d >>= 1) work[k] += __shfl_xor(work[k], d);
-        if (lane == 0) s_work[k][wave] = work[k];
-    }
-    const bool no_rows = __syncthreads_or(bad & 2);      // rows that are no partition: nothing is computed
-    int chunk[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        int64_t all = 0;
-        for (int w = 0; w < WAVES; ++w) all += s_work[k][w];
-        const int64_t target = k ? kLongTarget : kShortTarget, least = k ? kLongMinSplit : kShortMinSplit;
-        const int64_t each = (all * p.c.n_heads + target - 1) / target;
-        chunk[k] = (int)min(((max(each, least) + 127) >> 7) << 7, (int64_t)1 << 30);
-    }
-    int32_t *array = p.plan + kPlanHead;
-    int base[4] = {0, 0, 0, 0};
-    for (int s0 = 0; s0 < p.b.n_seqs; s0 += kPlanThreads) {
-        const int s = s0 + threadIdx.x;
-        int own[4] = {0, 0, 0, 0}, v[4];
-        if (s < p.b.n_seqs) {
-            const Seq q = seq_of(p.b, s);
-            const int cut_s = splits_of(reach_of<kShortTile>(p, q), chunk[0]), cut_l = splits_of(reach_of<kLongTile>(p, q), chunk[1]);
-            own[0] = tiles_of<kShortTile>(p, q) * cut_s * p.c.n_heads;
-            own[1] = cut_s > 1 ? own[0] : 0;
-            own[2] = tiles_of<kLongTile>(p, q) * cut_l * p.c.n_heads;
-            own[3] = cut_l > 1 ? own[2] : 0;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[k] = own[k];
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int o = __shfl_up(v[k], d);
-                if (lane >= d) v[k] += o;
-            }
-            if (lane == 63) s_sum[k][wave] = v[k];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            int total = 0;
-            for (int w = 0; w < WAVES; ++w) {
-                if (w < wave) v[k] += s_sum[k][w];
-                total += s_sum[k][w];
-            }
-            if (s < p.b.n_seqs) array[(int64_t)k * p.b.n_seqs + s] = base[k] + v[k] - own[k];
-            base[k] += total;
-        }
-    }
-    if (threadIdx.x == 0) {
-        p.plan[kChunkShort] = no_rows ? INT_MAX : chunk[0];
-        p.plan[kChunkLong] = no_rows ? INT_MAX : chunk[1];
-        p.plan[kItemsShort] = no_rows ? 0 : base[0];
-        p.plan[kItemsLong] = no_rows ? 0 : base[2];
-    }
-}
+// The plan of batches of more than kInlineSeqs sequences.
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p) { make_plan<kPlanThreads>(p, p.plan, true); }
 
 // V^T of 16 columns and a block's 32 tokens, in the order of the second product (see above).
 template <int DP>
@@ -136,16 +61,18 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttnParams p)
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int col = lane & 15, grp = lane >> 4;
-    const Plan plan = plan_of<kRows>(p);
+    __shared__ int32_t s_plan[kInlineWords];
+    const int32_t *plan = plan_of(p, s_plan);
+    const int items = plan[kItemsShort];
     const int D = p.c.dim;
     uint16_t *s_v = reinterpret_cast<uint16_t *>(s_mem) + wave * kBlock * DP;
     float *s_o = reinterpret_cast<float *>(s_mem);
 
-    for (int n = blockIdx.x; n < plan.items; n += gridDim.x) {
+    for (int n = blockIdx.x; n < items; n += gridDim.x) {
         Seq q;
         const Item it = item_of<kRows>(p, plan, n, q);
         const int s = it.s, head = it.head, tile = it.tile, cut = it.cut;
-        const Range rg = range_of<kRows>(p, q, tile, plan.chunk);
+        const Range rg = range_of<kRows>(p, q, tile, plan[kChunkShort]);
         if (cut >= rg.splits) continue;
         const int lo = rg.lo + cut * rg.each, hi = min(rg.hi, lo + rg.each);
 
@@ -331,64 +258,83 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttnParams p)
     }
 }
 
-// Where the partial results of a row lie, -1 if its range was not cut.
-struct Parts {
-    int64_t first;
-    int cuts;
-};
-
-template <int R>
-__device__ inline Parts parts_of(const AttnParams &p, const Seq &q, int s, int r, int head)
-{
-    const Plan plan = plan_of<R>(p);
-    const int tile = r / R;
-    Parts x = {-1, range_of<R>(p, q, tile, plan.chunk).splits};
-    if (x.cuts > 1) {
-        const int cuts = splits_of(reach_of<R>(p, q), plan.chunk);
-        const int slot = plan.slot[s] + tile * cuts * p.c.n_heads + head;
-        x.first = (int64_t)slot * R + r - tile * R;
-    }
-    return x;
-}
-
-// Joins the cuts of rows whose range was cut: a wave per row and head, by the rule of the running softmax.
+// Joins the cuts of rows whose range was cut, by the rule of the running softmax: a wave per row and head.  Lanes look at
+// 64 cuts' maxima and sums at a time, and hand their factors on to the lanes that add up the outputs: DP / 4 lanes take one
+// cut's 16 bytes each, eight cuts are on their way at once.
+template <int DP>
 __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
 {
-    const int lane = threadIdx.x & 63;
-    const int n = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    if (n >= p.b.n_rows * p.heads) return;
-    const int t = n / p.heads, qh = n - t * p.heads;
-    const int s = wave_find(p.b.row_start, p.b.n_seqs, t);
-    const Seq q = seq_of(p.b, s);
-    const int head = qh / p.group;
-    const int i = t - p.b.row_start[s];
-    if (i < 0 || i >= q.rows) return;
-    const int r = i * p.group + qh - head * p.group;
-    const bool is_short = q.rows * p.group <= p.short_limit;
-    const Parts parts = is_short ? parts_of<kShortTile>(p, q, s, r, head) : parts_of<kLongTile>(p, q, s, r, head);
-    if (parts.first < 0) return;
-    const float *ml = is_short ? p.part_ml : p.long_ml, *po = is_short ? p.part_o : p.long_o;
-    const int64_t step = (int64_t)p.c.n_heads * (is_short ? kShortTile : kLongTile);
-    float m = -INFINITY;
-    for (int c = 0; c < parts.cuts; ++c) m = fmaxf(m, ml[(parts.first + c * step) * 2]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
-    const int d = lane * 4;
-    for (int c = 0; c < parts.cuts; ++c) {
-        const int64_t at = parts.first + c * step;
-        const float f = __builtin_amdgcn_exp2f((ml[at * 2] - ref) * p.scale_log2);
-        total += f * ml[at * 2 + 1];
-        if (d < p.c.dim) sum += ld16f(po + at * p.c.dim + d) * f;
+    constexpr int LANES = DP / 4, SETS = 64 / LANES, DEEP = 8;
+    __shared__ int32_t s_plan[kInlineWords];
+    const int32_t *plan = plan_of(p, s_plan);
+    const int units = plan[kJoinUnits];
+    const int lane = threadIdx.x & 63, set = lane / LANES, d = (lane % LANES) * 4;
+    for (int u = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); u < units; u += gridDim.x * 4) {
+        const int32_t *base = plan + kPlanHead + kBaseJoin * p.b.n_seqs;
+        const int s = wave_find(base, p.b.n_seqs, u);
+        const int left = u - base[s];
+        const int i = left / p.heads, qh = left - i * p.heads;
+        const Seq q = seq_of(p.b, s);
+        const int head = qh / p.group;
+        const int r = i * p.group + qh - head * p.group;
+        const bool is_short = tiles_of<kShortTile>(p, q) > 0;
+        const int R = is_short ? kShortTile : kLongTile, chunk = plan[is_short ? kChunkShort : kChunkLong];
+        const int tile = r / R;
+        const int cuts = is_short ? range_of<kShortTile>(p, q, tile, chunk).splits : range_of<kLongTile>(p, q, tile, chunk).splits;
+        if (cuts == 1) continue;
+        const int most = splits_of(is_short ? reach_of<kShortTile>(p, q) : reach_of<kLongTile>(p, q), chunk);
+        const int slot = plan[kPlanHead + (is_short ? kSlotShort : kSlotLong) * p.b.n_seqs + s] + tile * most * p.c.n_heads + head;
+        const int64_t first = (int64_t)slot * R + r - tile * R, step = (int64_t)p.c.n_heads * R;
+        const float *ml = is_short ? p.part_ml : p.long_ml, *po = is_short ? p.part_o : p.long_o;
+        const int64_t t = p.b.row_start[s] + i;
+
+        float m = -INFINITY, total = 0.f;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int c0 = 0; c0 < cuts; c0 += 64) {
+            const bool have = c0 + lane < cuts;
+            const float *at = ml + (first + min(c0 + lane, cuts - 1) * step) * 2;
+            const float own_m = have ? at[0] : -INFINITY, own_l = have ? at[1] : 0.f;
+            float now = own_m;
+#pragma unroll
+            for (int x = 32; x; x >>= 1) now = fmaxf(now, __shfl_xor(now, x));
+            now = fmaxf(m, now);
+            const float ref = now == -INFINITY ? 0.f : now;
+            const float keep = __builtin_amdgcn_exp2f((m - ref) * p.scale_log2);
+            const float f = __builtin_amdgcn_exp2f((own_m - ref) * p.scale_log2);
+            float part = f * own_l;
+#pragma unroll
+            for (int x = 32; x; x >>= 1) part += __shfl_xor(part, x);
+            total = total * keep + part;
+            sum *= keep;
+            m = now;
+            const int n = min(64, cuts - c0);
+            for (int c = 0; c < n; c += SETS * DEEP) {
+                f32x4 x[DEEP];
+#pragma unroll
+                for (int k = 0; k < DEEP; ++k) {
+                    const int cc = c + k * SETS + set;
+                    x[k] = cc < n && d < p.c.dim ? ld16f(po + (first + (c0 + cc) * step) * p.c.dim + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+#pragma unroll
+                for (int k = 0; k < DEEP; ++k) sum += x[k] * __shfl(f, min(c + k * SETS + set, 63));
+            }
+        }
+#pragma unroll
+        for (int x = LANES; x < 64; x <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], x);
+        const float norm = total == 0.f ? 0.f : 1.f / total;
+        if (set == 0 && d < p.c.dim) {
+            u32x2 b;
+            b[0] = pack_bf16_rne(sum[0] * norm, sum[1] * norm);
+            b[1] = pack_bf16_rne(sum[2] * norm, sum[3] * norm);
+            *reinterpret_cast<u32x2 *>(p.out + t * p.ldo + (int64_t)qh * p.c.dim + d) = b;
+        }
+        if (lane == 0 && p.lse) {
+            const float ref = m == -INFINITY ? 0.f : m;
+            p.lse[t * p.heads + qh] = total == 0.f ? -INFINITY : (ref * p.scale_log2 + __builtin_amdgcn_logf(total)) * kLn2;
+        }
     }
-    const float norm = total == 0.f ? 0.f : 1.f / total;
-    if (d < p.c.dim) {
-        u32x2 b;
-        b[0] = pack_bf16_rne(sum[0] * norm, sum[1] * norm);
-        b[1] = pack_bf16_rne(sum[2] * norm, sum[3] * norm);
-        *reinterpret_cast<u32x2 *>(p.out + t * p.ldo + (int64_t)qh * p.c.dim + d) = b;
-    }
-    if (lane == 0 && p.lse) p.lse[(int64_t)t * p.heads + qh] = total == 0.f ? -INFINITY : (ref * p.scale_log2 + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -423,7 +369,7 @@ Ws ws_of(int n_seqs, const Kinds &k, int dim)
 {
     Ws w;
     w.plan = 0;
-    w.short_ml = up256((kPlanHead + 4 * (size_t)n_seqs) * 4);
+    w.short_ml = up256((kPlanHead + kPlanArrays * (size_t)n_seqs) * 4);
     w.short_o = w.short_ml + up256(k.has_short ? 2 * (size_t)kShortTarget * kShortTile * 8 : 0);
     w.long_ml = w.short_o + up256(k.has_short ? 2 * (size_t)kShortTarget * kShortTile * dim * 4 : 0);
     w.long_o = w.long_ml + up256(k.has_long ? 2 * (size_t)kLongTarget * kLongTile * 8 : 0);
@@ -449,7 +395,7 @@ hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s
     p.long_ml = reinterpret_cast<float *>(w + at.long_ml);
     p.long_o = reinterpret_cast<float *>(w + at.long_o);
     p.short_limit = k.limit;
-    hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+    if (p.b.n_seqs > kInlineSeqs) hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
     if (k.has_long) {
         const hipError_t e = launch_attend_long(p, (int)std::min<int64_t>(k.long_items, INT_MAX), s);
         if (e != hipSuccess) return e;
@@ -460,8 +406,15 @@ hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s
         else if (p.c.dim <= 128) hipLaunchKernelGGL(attend_kernel<128>, grid, block, 0, s, p);
         else hipLaunchKernelGGL(attend_kernel<256>, grid, block, 0, s, p);
     }
-    const int64_t waves = (int64_t)p.b.n_rows * p.heads;
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, p);
+    if (std::min<int64_t>(p.b.tokens_max, p.window ? (int64_t)p.window + kLongTile : INT_MAX) > kShortMinSplit) {
+        // of short tiles at most kShortTarget can be cut, of long ones kLongTarget
+        const int64_t units = std::min<int64_t>((int64_t)p.b.n_rows * p.heads, (k.has_short ? kShortTarget * kShortTile : 0) +
+                                                                                  (k.has_long ? kLongTarget * kLongTile : 0));
+        const dim3 grid((unsigned)std::min<int64_t>((units + 3) / 4, 1024)), block(256);
+        if (p.c.dim <= 64) hipLaunchKernelGGL(join_kernel<64>, grid, block, 0, s, p);
+        else if (p.c.dim <= 128) hipLaunchKernelGGL(join_kernel<128>, grid, block, 0, s, p);
+        else hipLaunchKernelGGL(join_kernel<256>, grid, block, 0, s, p);
+    }
     return hipGetLastError();
 }
 

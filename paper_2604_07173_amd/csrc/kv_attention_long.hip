@@ -71,13 +71,14 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int D = FULL ? DP : p.c.dim;
-    const Plan plan = plan_of<kRows>(p);
+    __shared__ int32_t s_plan[kInlineWords];
+    const int32_t *plan = plan_of(p, s_plan);
     const int n = blockIdx.x;
-    if (n >= plan.items) return;
+    if (n >= plan[kItemsLong]) return;
     Seq q;
     const Item it = item_of<kRows>(p, plan, n, q);
     const int tile = it.cuts > 1 ? it.tile : tiles_of<kRows>(p, q) - 1 - it.tile;        // long ranges first
-    const Range rg = range_of<kRows>(p, q, tile, plan.chunk);
+    const Range rg = range_of<kRows>(p, q, tile, plan[kChunkLong]);
     if (it.cut >= rg.splits) return;
     const int lo = rg.lo + it.cut * rg.each, hi = min(rg.hi, lo + rg.each);
 
