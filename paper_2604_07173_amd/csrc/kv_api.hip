@@ -271,6 +271,9 @@ int lora_kv_attention(const lora_kv_cache *cache, int layer, const lora_kv_batch
     p.scale_log2 = (float)(scale * 1.4426950408889634);
     p.heads = n_heads;
     p.group = n_heads / cache->n_heads;
+    p.group_div = fast_div(p.group);
+    p.kv_div = fast_div(cache->n_heads);
+    p.heads_div = fast_div(n_heads);
     p.causal = causal != 0;
     p.window = window < p.b.tokens_max ? window : 0;     // as wide as the longest sequence: no window
     LORA_HIP(launch_attention(p, batch->max_rows, ws, static_cast<hipStream_t>(stream)));

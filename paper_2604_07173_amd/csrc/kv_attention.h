@@ -1,27 +1,35 @@
-// What the two attention kernels share: work items, and the plan that cuts long ranges.
+// What the two attention kernels share: tiles, and the plan that divides the work.
 //
-// A tile is R rows of one sequence and one key/value head: row r is query head r % group of new token r / group,
-// so the heads that share K and V share their loads.  Sequences with few rows go in tiles of kShortTile
-// (kv_attention.hip), the others in tiles of kLongRows (kv_attention_long.hip).  A work item is a tile and a
-// range of its visible tokens; the plan cuts long ranges into items that run in parallel, and join_kernel
-// joins their results.
+// A tile is a number of rows of one sequence and one key/value head: row r is query head r % group of new token
+// r / group, so the heads that share K and V share their loads.  Sequences with few rows go in tiles of 16 or 32 rows
+// (kShort, kv_attention.hip), the others in tiles of kLongTile (kLong, kv_attention_long.hip).
+//
+// Short tiles are bound by the reading of K and V.  All their tokens, in units of 128 per tile, form one line, and every
+// workgroup takes an equal stretch of it, whatever the lengths are: several tiles, or a part of a long one.  Tiles that
+// lie across the end of a stretch leave partial results, two at most per workgroup, which join_kernel joins.
+//
+// Long tiles are work items of their own; where there are few, their tokens are cut evenly into several items.
 #pragma once
 #include "kv_device.h"
 
 namespace lora {
 
-constexpr int kShortTile = 16, kLongTile = 128;   // rows
-constexpr int kShortTarget = 2048, kLongTarget = 512;   // work items that fill the chip: longer ranges are cut into about as many
-constexpr int kShortMinSplit = 256, kLongMinSplit = 512;   // tokens of a cut range at least
+constexpr int kLongTile = 128;           // rows
+constexpr int kUnitShift = 7;            // a unit is 128 tokens: a step of a workgroup's four waves
+constexpr float kMostUnits = 1 << 29;    // on the line; units are doubled until there are no more
+constexpr int kMostBlocks = 768;         // workgroups of short tiles: three on every CU
+constexpr int kLongTarget = 512;         // items of long tiles that fill the chip
+constexpr int kLongMinSplit = 512;       // tokens of a cut range at least
 constexpr int kShortLimit = 64;          // rows x group up to which a sequence goes in short tiles
 constexpr float kLn2 = 0.6931471805599453f;
-
 constexpr int kInlineSeqs = 256;         // sequences up to which every workgroup makes the plan for itself, in LDS: one launch less
 
-// The plan: a head of kPlanHead words, then kPlanArrays arrays over the sequences: work items and partial results before
-// each sequence, of short and of long tiles, and rows x heads to join.
-enum { kChunkShort, kChunkLong, kItemsShort, kItemsLong, kJoinUnits, kPlanHead = 8 };
-enum { kBaseShort, kSlotShort, kBaseLong, kSlotLong, kBaseJoin, kPlanArrays };
+enum Kind { kShort, kLong };
+
+// The plan: a head of kPlanHead words, then kPlanArrays arrays over the sequences: units of short tiles before each
+// sequence, work items and partial results of long tiles, and rows x heads of long tiles to join.
+enum { kUnits, kShare, kUnitTokens, kChunk, kItems, kJoinUnits, kPlanHead = 8 };
+enum { kBaseUnit, kBaseItem, kBaseSlot, kBaseJoin, kPlanArrays };
 constexpr int kInlineWords = kPlanHead + kPlanArrays * kInlineSeqs;
 
 struct Seq {
@@ -38,159 +46,187 @@ __device__ inline Seq seq_of(const KvRows &b, int s)
     return q;
 }
 
-// Tiles of R rows that the sequence has (none if it goes in the other kind).
-template <int R>
+template <Kind K>
+__device__ inline int tile_rows(const AttnParams &p) { return K == kShort ? 1 << p.short_shift : kLongTile; }
+
+// Tiles that the sequence has of this kind.
+template <Kind K>
 __device__ inline int tiles_of(const AttnParams &p, const Seq &q)
 {
     const int n = q.rows * p.group;
-    if ((n <= p.short_limit) != (R == kShortTile)) return 0;
-    return (n + R - 1) / R;
+    if ((n <= p.short_limit) != (K == kShort)) return 0;
+    return K == kShort ? (n + (1 << p.short_shift) - 1) >> p.short_shift : (n + kLongTile - 1) / kLongTile;
 }
 
 // Most tokens that a tile of the sequence sees.
-template <int R>
+template <Kind K>
 __device__ inline int reach_of(const AttnParams &p, const Seq &q)
 {
     if (!p.window) return q.len;
-    const int64_t most = (int64_t)p.window - 1 + min(q.rows, R / p.group + 2);
-    return (int)min((int64_t)q.len, most);
+    const int most = p.window - 1 + min(q.rows, tile_rows<K>(p) / p.group_div + 2);
+    return min(q.len, most);
 }
 
 __device__ inline int splits_of(int reach, int chunk) { return reach <= chunk ? 1 : (reach + chunk - 1) / chunk; }
 
-// A tile's tokens [lo, hi), into how many items they are cut, and the tokens of each.
+__device__ inline int units_of(int reach, int shift) { return max(1, (reach + (1 << shift) - 1) >> shift); }
+
+// Tokens of a unit, as a power of two.  `units`: of 128 tokens, all of the line.
+__device__ inline int unit_shift_of(float units)
+{
+    int shift = kUnitShift;
+    for (; units > kMostUnits && shift < 30; units *= 0.5f) ++shift;
+    return shift;
+}
+
+// A tile's tokens [lo, hi).
 struct Range {
-    int lo, hi, splits, each;
+    int lo, hi;
 };
 
-template <int R>
-__device__ inline Range range_of(const AttnParams &p, const Seq &q, int tile, int chunk)
+template <Kind K>
+__device__ inline Range range_of(const AttnParams &p, const Seq &q, int tile)
 {
-    const int i0 = tile * R / p.group, i1 = min(q.rows - 1, (tile * R + R - 1) / p.group);
+    const int R = tile_rows<K>(p);
+    const int i0 = tile * R / p.group_div, i1 = min(q.rows - 1, (tile * R + R - 1) / p.group_div);
     Range r;
     r.hi = p.causal ? max(0, min(q.len, q.pos0 + i1 + 1)) : q.len;
     r.lo = p.window ? max(0, q.pos0 + i0 - p.window + 1) : 0;
     if (r.lo >= r.hi) r.lo = r.hi = 0;
-    r.splits = splits_of(r.hi - r.lo, chunk);
-    // evenly, in multiples of 64, as the chunk is one: no cut is empty, as splits - 1 chunks are not enough
-    r.each = r.splits == 1 ? r.hi - r.lo : ((r.hi - r.lo + r.splits - 1) / r.splits + 63) >> 6 << 6;
     return r;
 }
 
-// Makes the plan with a workgroup of THREADS, into LDS or the workspace: cuts the ranges so that all work items of a kind
-// take about as long.  Rows that are no partition of the batch's give no work at all.
-template <int THREADS>
-__device__ inline void make_plan(const AttnParams &p, int32_t *plan, bool report)
+// Tokens of an item of a cut tile.  `work`: tokens that all long tiles of a key/value head see.  A little more than the
+// even share, so that the number of cut items stays below twice the target however it was rounded; a tile is
+// only cut where that fills the chip better.
+__device__ inline int chunk_of(const AttnParams &p, float work)
 {
-    constexpr int WAVES = THREADS / 64;
-    __shared__ int64_t s_work[2][WAVES];
-    __shared__ int s_sum[kPlanArrays][WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n = p.b.n_seqs;
-    int64_t work[2] = {0, 0};
-    unsigned bad = 0;
-    for (int s = tid; s < n; s += THREADS) {
-        const Seq q = seq_of(p.b, s);
-        if (p.b.seq_len[s] != q.len) bad |= 1;
-        const int first = p.b.row_start[s], end = p.b.row_start[s + 1];
-        if (first < 0 || end < first || end > p.b.n_rows || (s == 0 && first != 0) || (s == n - 1 && end != p.b.n_rows)) bad |= 2;
-        work[0] += (int64_t)tiles_of<kShortTile>(p, q) * reach_of<kShortTile>(p, q);
-        work[1] += (int64_t)tiles_of<kLongTile>(p, q) * reach_of<kLongTile>(p, q);
-    }
-    if (bad && report) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        work[0] += __shfl_xor(work[0], d);
-        work[1] += __shfl_xor(work[1], d);
-    }
-    if (lane == 0) s_work[0][wave] = work[0], s_work[1][wave] = work[1];
-    const bool no_rows = __syncthreads_or(bad & 2);
-    int chunk[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        int64_t all = 0;
-        for (int w = 0; w < WAVES; ++w) all += s_work[k][w];
-        const int64_t target = k ? kLongTarget : kShortTarget, least = k ? kLongMinSplit : kShortMinSplit;
-        const int64_t each = (all * p.c.n_heads + target - 1) / target;
-        chunk[k] = (int)min(((max(each, least) + 127) >> 7) << 7, (int64_t)1 << 30);
-    }
-    int base[kPlanArrays] = {};
-    for (int s0 = 0; s0 < n; s0 += THREADS) {
-        const int s = s0 + tid;
-        int own[kPlanArrays] = {}, v[kPlanArrays];
-        if (s < n && !no_rows) {
-            const Seq q = seq_of(p.b, s);
-            const int cut_s = splits_of(reach_of<kShortTile>(p, q), chunk[0]), cut_l = splits_of(reach_of<kLongTile>(p, q), chunk[1]);
-            const int tiles_s = tiles_of<kShortTile>(p, q), tiles_l = tiles_of<kLongTile>(p, q);
-            own[kBaseShort] = tiles_s * cut_s * p.c.n_heads;
-            own[kSlotShort] = cut_s > 1 ? own[kBaseShort] : 0;
-            own[kBaseLong] = tiles_l * cut_l * p.c.n_heads;
-            own[kSlotLong] = cut_l > 1 ? own[kBaseLong] : 0;
-            own[kBaseJoin] = (tiles_s ? cut_s : cut_l) > 1 ? q.rows * p.heads : 0;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kPlanArrays; ++k) v[k] = own[k];
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-            for (int k = 0; k < kPlanArrays; ++k) {
-                const int o = __shfl_up(v[k], d);
-                if (lane >= d) v[k] += o;
-            }
-        if (lane == 63)
-#pragma unroll
-            for (int k = 0; k < kPlanArrays; ++k) s_sum[k][wave] = v[k];
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kPlanArrays; ++k) {
-            int total = 0;
-            for (int w = 0; w < WAVES; ++w) {
-                if (w < wave) v[k] += s_sum[k][w];
-                total += s_sum[k][w];
-            }
-            if (s < n) plan[kPlanHead + k * n + s] = base[k] + v[k] - own[k];
-            base[k] += total;
-        }
-    }
-    if (tid == 0) {
-        plan[kChunkShort] = chunk[0];
-        plan[kChunkLong] = chunk[1];
-        plan[kItemsShort] = base[kBaseShort];
-        plan[kItemsLong] = base[kBaseLong];
-        plan[kJoinUnits] = base[kBaseJoin];
-    }
-    __syncthreads();
+    const float each = work * (float)p.c.n_heads * (1.25f / kLongTarget);
+    return each < (float)kLongMinSplit ? kLongMinSplit : each > 1e9f ? 1 << 30 : ((int)each + 128) >> 7 << 7;
 }
 
-// The plan of a workgroup of 256: made in s_plan, or what a launch before has left in the workspace.
+// Tokens of each cut, evenly, in multiples of 64, as the chunk is one: no cut is empty, as splits - 1 chunks are not enough.
+__device__ inline int cut_of(const Range &r, int splits)
+{
+    return splits == 1 ? r.hi - r.lo : ((r.hi - r.lo + splits - 1) / splits + 63) >> 6 << 6;
+}
+
+// What a sequence adds to the plan's arrays.
+__device__ inline void plan_entry(const AttnParams &p, const Seq &q, int shift, int chunk, int (&own)[kPlanArrays])
+{
+    const int tiles = tiles_of<kLong>(p, q);
+    const int cuts = splits_of(reach_of<kLong>(p, q), chunk);
+    own[kBaseUnit] = tiles_of<kShort>(p, q) * p.c.n_heads * units_of(reach_of<kShort>(p, q), shift);
+    own[kBaseItem] = tiles * cuts * p.c.n_heads;
+    own[kBaseSlot] = cuts > 1 ? own[kBaseItem] : 0;
+    own[kBaseJoin] = cuts > 1 && tiles ? q.rows * p.heads : 0;
+}
+
+__device__ inline void plan_head(const AttnParams &p, int32_t *plan, int shift, int chunk, const int (&sum)[kPlanArrays])
+{
+    plan[kUnits] = sum[kBaseUnit];
+    plan[kShare] = max(1, (sum[kBaseUnit] + p.short_blocks - 1) / p.short_blocks);
+    plan[kUnitTokens] = shift;
+    plan[kChunk] = chunk;
+    plan[kItems] = sum[kBaseItem];
+    plan[kJoinUnits] = sum[kBaseJoin];
+}
+
+// Rows of sequence s that are no part of a partition of the batch's (2), a length that the table cannot hold (1).
+__device__ inline unsigned faults_of(const KvRows &b, int s)
+{
+    const int first = b.row_start[s], end = b.row_start[s + 1], len = b.seq_len[s];
+    unsigned bad = len < 0 || len > b.tokens_max;
+    if (first < 0 || end < first || end > b.n_rows || (s == 0 && first != 0) || (s == b.n_seqs - 1 && end != b.n_rows)) bad |= 2;
+    return bad;
+}
+
+// The plan of up to kInlineSeqs sequences, by one wave: lane l takes the sequences l * each .. of the batch.
+__device__ inline void make_plan(const AttnParams &p, int32_t *plan)
+{
+    constexpr int MOST = kInlineSeqs / 64;
+    const int lane = threadIdx.x & 63, n = p.b.n_seqs, each = (n + 63) >> 6;
+    Seq q[MOST];
+    unsigned bad = 0;
+    float work = 0.f;
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) {
+        const int s = lane * each + k;
+        q[k] = Seq{0, 0, 0};
+        if (k < each && s < n) {
+            q[k] = seq_of(p.b, s);
+            bad |= faults_of(p.b, s);
+        }
+    }
+    float units = 0.f;
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) units += (float)(tiles_of<kShort>(p, q[k]) * p.c.n_heads) * (float)units_of(reach_of<kShort>(p, q[k]), kUnitShift);
+    const int shift = unit_shift_of(last_lane(wave_scan(units)));
+    int chunk = 1 << 30;
+    if (p.long_o) {
+#pragma unroll
+        for (int k = 0; k < MOST; ++k) work += (float)tiles_of<kLong>(p, q[k]) * (float)reach_of<kLong>(p, q[k]);
+        chunk = chunk_of(p, last_lane(wave_scan(work)));
+    }
+    int own[MOST][kPlanArrays] = {}, sum[kPlanArrays] = {};
+    if (!__any(bad & 2)) {                // rows that are no partition: no work at all
+#pragma unroll
+        for (int k = 0; k < MOST; ++k) {
+            if (k >= each) break;
+            plan_entry(p, q[k], shift, chunk, own[k]);
+#pragma unroll
+            for (int a = 0; a < kPlanArrays; ++a) sum[a] += own[k][a];
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < kPlanArrays; ++a) {
+        const int upto = wave_scan(sum[a]);
+        int before = upto - sum[a];
+        sum[a] = upto;                    // lane 63's is the total
+#pragma unroll
+        for (int k = 0; k < MOST; ++k) {
+            const int s = lane * each + k;
+            if (k < each && s < n) plan[kPlanHead + a * n + s] = before;
+            before += own[k][a];
+        }
+    }
+    if (lane == 63) plan_head(p, plan, shift, chunk, sum);
+    if (bad && blockIdx.x == 0) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
+}
+
+// The plan: made in s_plan by the workgroup's first wave, or what a launch before has left in the workspace.
 __device__ inline const int32_t *plan_of(const AttnParams &p, int32_t *s_plan)
 {
     if (p.b.n_seqs > kInlineSeqs) return p.plan;
-    make_plan<256>(p, s_plan, blockIdx.x == 0);
+    if (threadIdx.x < 64) make_plan(p, s_plan);
+    __syncthreads();
     return s_plan;
 }
 
-struct Item {
-    int s, head, tile, cut, cuts, slot;
+// The sequence that entry n of one of the plan's arrays belongs to.
+__device__ inline int seq_at(const AttnParams &p, const int32_t *base, int n)
+{
+    return __builtin_amdgcn_readfirstlane(p.b.n_seqs == 1 ? 0 : wave_find(base, p.b.n_seqs, n));
+}
+
+// A tile on the line of units.
+struct Place {
+    int s, head, tile, start, units;     // start: the tile's first unit on the line
 };
 
-// Work item n: the cuts of a tile lie n_heads apart, tiles behind each other.
-template <int R>
-__device__ inline Item item_of(const AttnParams &p, const int32_t *plan, int n, Seq &q)
+__device__ inline Place place_of(const AttnParams &p, const int32_t *plan, int unit, Seq &q)
 {
-    const int32_t *base = plan + kPlanHead + (R == kShortTile ? kBaseShort : kBaseLong) * p.b.n_seqs;
-    Item it;
-    it.s = wave_find(base, p.b.n_seqs, n);
-    q = seq_of(p.b, it.s);
-    const int left = n - base[it.s];
-    it.slot = base[p.b.n_seqs + it.s] + left;
-    const int pair = left / p.c.n_heads;
-    it.head = left - pair * p.c.n_heads;
-    it.cuts = splits_of(reach_of<R>(p, q), plan[R == kShortTile ? kChunkShort : kChunkLong]);
-    it.tile = pair / it.cuts;
-    it.cut = pair - it.tile * it.cuts;
-    return it;
+    const int32_t *base = plan + kPlanHead + kBaseUnit * p.b.n_seqs;
+    Place x;
+    x.s = seq_at(p, base, unit);
+    q = seq_of(p.b, x.s);
+    x.units = units_of(reach_of<kShort>(p, q), plan[kUnitTokens]);
+    const int before = base[x.s];
+    const int pair = x.units == 1 ? unit - before : (unit - before) / x.units;
+    x.start = before + pair * x.units;
+    x.tile = pair / p.kv_div;
+    x.head = pair - x.tile * p.c.n_heads;
+    return x;
 }
 
 // Any of eight bf16 that is no finite number.

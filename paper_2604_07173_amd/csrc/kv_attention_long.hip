@@ -74,25 +74,34 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     __shared__ int32_t s_plan[kInlineWords];
     const int32_t *plan = plan_of(p, s_plan);
     const int n = blockIdx.x;
-    if (n >= plan[kItemsLong]) return;
-    Seq q;
-    const Item it = item_of<kRows>(p, plan, n, q);
-    const int tile = it.cuts > 1 ? it.tile : tiles_of<kRows>(p, q) - 1 - it.tile;        // long ranges first
-    const Range rg = range_of<kRows>(p, q, tile, plan[kChunkLong]);
-    if (it.cut >= rg.splits) return;
-    const int lo = rg.lo + it.cut * rg.each, hi = min(rg.hi, lo + rg.each);
+    if (n >= plan[kItems]) return;
+    // the cuts of a tile lie n_heads apart, tiles behind each other, those with the longest ranges first
+    const int32_t *base = plan + kPlanHead + kBaseItem * p.b.n_seqs;
+    const int seq = seq_at(p, base, n);
+    const Seq q = seq_of(p.b, seq);
+    const int left = n - base[seq];
+    const int pair = left / p.kv_div, head = left - pair * p.c.n_heads;
+    const int cuts = splits_of(reach_of<kLong>(p, q), plan[kChunk]);
+    const int turn_no = cuts == 1 ? pair : pair / cuts, cut = pair - turn_no * cuts;
+    const int tile = tiles_of<kLong>(p, q) - 1 - turn_no;
+    const Range rg = range_of<kLong>(p, q, tile);
+    const int splits = splits_of(rg.hi - rg.lo, plan[kChunk]);
+    if (cut >= splits) return;
+    const int each = cut_of(rg, splits);
+    const int lo = rg.lo + cut * each, hi = min(rg.hi, lo + each);
+    const int slot = plan[kPlanHead + kBaseSlot * p.b.n_seqs + seq] + (tile * cuts + cut) * p.c.n_heads + head;
 
     // this lane's row, and the tokens that it, some row and every row of its wave see
     const int r0 = tile * kRows + wave * 32;
     const int n_rows = q.rows * p.group;
     const int r = r0 + col;
-    const int i = r / p.group, g = r - i * p.group;
+    const int i = r / p.group_div, g = r - i * p.group;
     const bool real = r < n_rows;
-    const int64_t t = p.b.row_start[it.s] + i;
-    const int qh = it.head * p.group + g;
+    const int64_t t = p.b.row_start[seq] + i;
+    const int qh = head * p.group + g;
     const int see_hi = !real ? 0 : p.causal ? min(hi, q.pos0 + i + 1) : hi;
     const int see_lo = p.window ? max(lo, q.pos0 + i - p.window + 1) : lo;
-    const int first_i = r0 / p.group, last_i = min(q.rows - 1, (r0 + 31) / p.group);
+    const int first_i = r0 / p.group_div, last_i = min(q.rows - 1, (r0 + 31) / p.group_div);
     const int any_hi = r0 >= n_rows ? 0 : p.causal ? min(hi, q.pos0 + last_i + 1) : hi;
     const int any_lo = p.window ? max(lo, q.pos0 + first_i - p.window + 1) : lo;
     const int all_hi = p.causal ? min(hi, q.pos0 + first_i + 1) : hi;
@@ -128,9 +137,9 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
 
     // This wave's loads of a step: load j covers rows (wave * NL + j) * RPL + lane / CH.  Lane j of every CH lanes looks up
     // the page of load j's row and hands the place to the others; a lane fetches the piece that belongs at its place.
-    const int32_t *table = p.b.table + (int64_t)it.s * p.b.max_pages;
+    const int32_t *table = p.b.table + (int64_t)seq * p.b.max_pages;
     const int place_mask = (1 << p.c.page_shift) - 1;
-    const uint16_t *kbase = p.c.k + it.head * p.c.head_stride, *vbase = p.c.v + it.head * p.c.head_stride;
+    const uint16_t *kbase = p.c.k + head * p.c.head_stride, *vbase = p.c.v + head * p.c.head_stride;
     const int my_row = (wave * NL + (lane & (NL - 1))) * RPL + lane / CH;
     int piece[2];                         // of even and of odd loads
 #pragma unroll
@@ -289,7 +298,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     l += other_half(l);
     if (!real) return;
     const float ref = ms == -INFINITY ? 0.f : ms;
-    if (rg.splits == 1) {
+    if (splits == 1) {
         const float norm = l == 0.f ? 0.f : 1.f / l;
         uint16_t *out = p.out + t * p.ldo + (int64_t)qh * D;
 #pragma unroll
@@ -305,7 +314,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
             }
         if (p.lse && half == 0) p.lse[t * p.heads + qh] = l == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l)) * kLn2;
     } else {
-        const int64_t at = (int64_t)it.slot * kRows + wave * 32 + col;
+        const int64_t at = (int64_t)slot * kRows + wave * 32 + col;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll

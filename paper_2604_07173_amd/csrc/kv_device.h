@@ -22,6 +22,29 @@ __device__ inline int wave_find(const int32_t *a, int n, int x)
     return lo;
 }
 
+// Inclusive prefix sum over the wave, in six steps of the lanes' own exchange paths (no trip through LDS).
+template <class T>
+__device__ inline T wave_scan(T x)
+{
+    static_assert(sizeof(T) == 4, "one register");
+#define LORA_SCAN_STEP(CTRL, ROWS) \
+    x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
+    LORA_SCAN_STEP(0x111, 0xf)            // row_shr 1, 2, 4, 8: within 16 lanes
+    LORA_SCAN_STEP(0x112, 0xf)
+    LORA_SCAN_STEP(0x114, 0xf)
+    LORA_SCAN_STEP(0x118, 0xf)
+    LORA_SCAN_STEP(0x142, 0xa)            // the last lane of rows 0 and 2 to rows 1 and 3
+    LORA_SCAN_STEP(0x143, 0xc)            // lane 31 to the upper half
+#undef LORA_SCAN_STEP
+    return x;
+}
+
+template <class T>
+__device__ inline T last_lane(T x)
+{
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
 // Page of a token by its table entry; an entry that is no page of the cache raises the status bit and is
 // replaced by a page that is, so that nothing is read out of bounds.
 __device__ inline int checked_page(int page, int n_pages, uint32_t *status)

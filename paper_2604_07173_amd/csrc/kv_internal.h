@@ -49,7 +49,10 @@ struct AttnParams {
     int64_t ldq, ldo;
     float scale_log2;             // scale / ln 2
     int heads, group, causal, window;
+    FastDiv group_div, kv_div, heads_div;
     int short_limit;              // rows x group of a sequence up to which it goes in short tiles
+    int short_shift;              // rows of a short tile, as a power of two
+    int short_blocks, join_blocks;   // workgroups that share the short tiles, and that join their parts
     int32_t *plan;                // device: see kv_attention.h
     float *part_o, *part_ml;      // partial results of short tiles whose range is cut: sums, and maximum and sum of weights
     float *long_o, *long_ml;
