@@ -78,14 +78,16 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     // the cuts of a tile lie n_heads apart, tiles behind each other, those with the longest ranges first
     const int32_t *base = plan + kPlanHead + kBaseItem * p.b.n_seqs;
     const int seq = seq_at(p, base, n);
-    const Seq q = seq_of(p.b, seq);
-    const int left = n - base[seq];
+    Seq q = seq_of(p.b, seq);
+    q.rows = uniform(q.rows), q.len = uniform(q.len), q.pos0 = q.len - q.rows;
+    const int left = uniform(n - base[seq]);
     const int pair = left / p.kv_div, head = left - pair * p.c.n_heads;
-    const int cuts = splits_of(reach_of<kLong>(p, q), plan[kChunk]);
+    const int chunk = uniform(plan[kChunk]);
+    const int cuts = splits_of(reach_of<kLong>(p, q), chunk);
     const int turn_no = cuts == 1 ? pair : pair / cuts, cut = pair - turn_no * cuts;
     const int tile = tiles_of<kLong>(p, q) - 1 - turn_no;
     const Range rg = range_of<kLong>(p, q, tile);
-    const int splits = splits_of(rg.hi - rg.lo, plan[kChunk]);
+    const int splits = splits_of(rg.hi - rg.lo, chunk);
     if (cut >= splits) return;
     const int each = cut_of(rg, splits);
     const int lo = rg.lo + cut * each, hi = min(rg.hi, lo + each);
@@ -183,10 +185,8 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int j = j0 + h * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-                    if (j < see_lo || j >= see_hi) s[h][e] = -INFINITY;
-                }
+                for (int e = 0; e < 16; ++e)
+                    if ((unsigned)(j0 + 4 * half - see_lo + h * 32 + 8 * (e >> 2) + (e & 3)) >= (unsigned)max(0, see_hi - see_lo)) s[h][e] = -INFINITY;
         }
         bf16x8 pf[4];
         float sum;
@@ -273,9 +273,10 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     };
     // the stage is full, and every wave has read what the next fetch overwrites
     const auto meet = [&] {
-        wait_loads<0>();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);            // vmcnt(0) lgkmcnt(0); the loads into LDS count as well
         __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
     const auto turn = [&](int j0, auto stage_c) {
         meet();

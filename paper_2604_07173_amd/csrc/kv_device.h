@@ -22,6 +22,9 @@ __device__ inline int wave_find(const int32_t *a, int n, int x)
     return lo;
 }
 
+// A value that is the same in every lane, where the compiler cannot know it.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // Inclusive prefix sum over the wave, in six steps of the lanes' own exchange paths (no trip through LDS).
 template <class T>
 __device__ inline T wave_scan(T x)
