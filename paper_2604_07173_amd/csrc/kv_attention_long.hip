@@ -175,11 +175,21 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
             return as_bf16x8(u32x4{a[0], a[1], b[0], b[1]});
         };
         f32x16 s[2] = {f32x16{}, f32x16{}};
+        __builtin_amdgcn_s_setprio(1);       // the wave beside this one forms weights meanwhile, or waits
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(lds_u32x4 *)(k_at[ks] + (AT + h * 32 * ROW))), qf[ks], s[h], 0, 0, 0);
+        // six operands are on their way ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int k = 0; k < KS * 2 - 6; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+        __builtin_amdgcn_s_setprio(0);
         const bool edge = j0 < all_lo || j0 + kTokens > all_hi;
         if (edge) {
 #pragma unroll
@@ -247,10 +257,19 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
             odd = __any(odd);
         }
         if (!odd) {
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_tile(k, d), pf[k], o[d], 0, 0, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+            for (int k = 0; k < 4 * DT - 4; ++k) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            __builtin_amdgcn_s_setprio(0);
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
