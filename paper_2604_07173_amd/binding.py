@@ -228,7 +228,9 @@ def load_library():
     if not os.path.exists(os.path.join(os.path.dirname(path), "_pycall.so")):
         raise RuntimeError("_pycall.so is not built; run `python -m paper_2604_07173_amd.build`")
     from . import _pycall as calls
-    calls.bind({name: C.cast(getattr(lib, name), vp).value for name in EXPORTED_SYMBOLS}, _stream)
+    addresses = {name: C.cast(getattr(lib, name), vp).value for name in EXPORTED_SYMBOLS}
+    calls.bind(addresses, _stream)
+    calls.bind_kv(addresses)
     _pycall = calls
     _lib = lib
     return lib
@@ -650,8 +652,9 @@ def _c(handle):
 
 def lora_rope_append(cache: KvCache, layer: int, batch: KvBatch, rope: Optional[Rope], q, ldq, k, ldk, v, ldv, q_out, ldqo,
                      n_heads: int, in_dtype=LORA_DTYPE_BF16, stream=None):
-    _check(load_library().lora_rope_append(_c(cache), layer, _c(batch), _c(rope), _addr(q), ldq, _addr(k), ldk, _addr(v), ldv,
-                                           _addr(q_out), ldqo, n_heads, in_dtype, _stream(stream)), "lora_rope_append")
+    rc = _calls().rope_append(cache, layer, batch, rope, q, ldq, k, ldk, v, ldv, q_out, ldqo, n_heads, in_dtype, stream)
+    if rc:
+        _check(rc, "lora_rope_append")
 
 
 def lora_kv_attention_ws_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int:
@@ -660,9 +663,9 @@ def lora_kv_attention_ws_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> 
 
 def lora_kv_attention(cache: KvCache, layer: int, batch: KvBatch, q, ldq, n_heads: int, out, ldo, lse, scale: float, ws,
                       causal: bool = True, window: int = 0, stream=None):
-    _check(load_library().lora_kv_attention(_c(cache), layer, _c(batch), _addr(q), ldq, n_heads, _addr(out), ldo, _addr(lse),
-                                            scale, int(causal), window, _addr(ws), ws.numel() * ws.element_size(),
-                                            _stream(stream)), "lora_kv_attention")
+    rc = _calls().kv_attention(cache, layer, batch, q, ldq, n_heads, out, ldo, lse, scale, causal, window, ws, stream)
+    if rc:
+        _check(rc, "lora_kv_attention")
 
 
 def lora_kv_moves_ws_bytes(n_pages: int, n_seqs: int) -> int:
@@ -695,16 +698,21 @@ class KvMoves:
 
 def lora_kv_plan(cache: KvCache, state: KvState, to: KvState, src, new_len, moves: KvMoves, stream=None):
     """src, new_len: int32 device tensors [n_seqs]."""
-    _check(load_library().lora_kv_plan(_c(cache), _c(state), _c(to), _addr(src), _addr(new_len), _c(moves), _stream(stream)),
-           "lora_kv_plan")
+    rc = _calls().kv_plan(cache, state, to, src, new_len, moves, stream)
+    if rc:
+        _check(rc, "lora_kv_plan")
 
 
 def lora_kv_compact(cache: KvCache, state: KvState, to: KvState, moves: KvMoves, stream=None):
-    _check(load_library().lora_kv_compact(_c(cache), _c(state), _c(to), _c(moves), _stream(stream)), "lora_kv_compact")
+    rc = _calls().kv_compact(cache, state, to, moves, stream)
+    if rc:
+        _check(rc, "lora_kv_compact")
 
 
 def lora_kv_copy_pages(cache: KvCache, moves: KvMoves, max_moves: int, stream=None):
-    _check(load_library().lora_kv_copy_pages(_c(cache), _c(moves), max_moves, _stream(stream)), "lora_kv_copy_pages")
+    rc = _calls().kv_copy_pages(cache, moves, max_moves, stream)
+    if rc:
+        _check(rc, "lora_kv_copy_pages")
 
 
 # ---- cache provisioning (include/lora_provision.h): host arrays in, numbers out ----------------

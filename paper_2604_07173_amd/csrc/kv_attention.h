@@ -27,20 +27,21 @@ constexpr int kInlineSeqs = 256;         // sequences up to which every workgrou
 enum Kind { kShort, kLong };
 
 // The plan: a head of kPlanHead words, then kPlanArrays arrays over the sequences: units of short tiles before each
-// sequence, work items and partial results of long tiles, and rows x heads of long tiles to join.
+// sequence, work items and partial results of long tiles, and rows x heads of long tiles to join; then the sequences
+// themselves.
 enum { kUnits, kShare, kUnitTokens, kChunk, kItems, kJoinUnits, kPlanHead = 8 };
-enum { kBaseUnit, kBaseItem, kBaseSlot, kBaseJoin, kPlanArrays };
+enum { kBaseUnit, kBaseItem, kBaseSlot, kBaseJoin, kPlanSums, kSeqRow0 = kPlanSums, kSeqRows, kSeqLen, kPlanArrays };
 constexpr int kInlineWords = kPlanHead + kPlanArrays * kInlineSeqs;
 
 struct Seq {
-    int rows, len, pos0;                 // new rows, length, position of the first new row
+    int row0, rows, len, pos0;           // first new row and their number, length, position of the first new row
 };
 
 __device__ inline Seq seq_of(const KvRows &b, int s)
 {
     Seq q;
-    const int first = min(max(0, b.row_start[s]), b.n_rows);
-    q.rows = max(0, min(b.row_start[s + 1], b.n_rows) - first);
+    q.row0 = min(max(0, b.row_start[s]), b.n_rows);
+    q.rows = max(0, min(b.row_start[s + 1], b.n_rows) - q.row0);
     q.len = min(max(0, b.seq_len[s]), b.tokens_max);
     q.pos0 = q.len - q.rows;
     return q;
@@ -112,7 +113,7 @@ __device__ inline int cut_of(const Range &r, int splits)
 }
 
 // What a sequence adds to the plan's arrays.
-__device__ inline void plan_entry(const AttnParams &p, const Seq &q, int shift, int chunk, int (&own)[kPlanArrays])
+__device__ inline void plan_entry(const AttnParams &p, const Seq &q, int shift, int chunk, int (&own)[kPlanSums])
 {
     const int tiles = tiles_of<kLong>(p, q);
     const int cuts = splits_of(reach_of<kLong>(p, q), chunk);
@@ -122,7 +123,7 @@ __device__ inline void plan_entry(const AttnParams &p, const Seq &q, int shift, 
     own[kBaseJoin] = cuts > 1 && tiles ? q.rows * p.heads : 0;
 }
 
-__device__ inline void plan_head(const AttnParams &p, int32_t *plan, int shift, int chunk, const int (&sum)[kPlanArrays])
+__device__ inline void plan_head(const AttnParams &p, int32_t *plan, int shift, int chunk, const int (&sum)[kPlanSums])
 {
     plan[kUnits] = sum[kBaseUnit];
     plan[kShare] = max(1, (sum[kBaseUnit] + p.short_blocks - 1) / p.short_blocks);
@@ -130,6 +131,23 @@ __device__ inline void plan_head(const AttnParams &p, int32_t *plan, int shift, 
     plan[kChunk] = chunk;
     plan[kItems] = sum[kBaseItem];
     plan[kJoinUnits] = sum[kBaseJoin];
+}
+
+__device__ inline void store_seq(int32_t *plan, int64_t n_seqs, int s, const Seq &q)
+{
+    plan[kPlanHead + kSeqRow0 * n_seqs + s] = q.row0;
+    plan[kPlanHead + kSeqRows * n_seqs + s] = q.rows;
+    plan[kPlanHead + kSeqLen * n_seqs + s] = q.len;
+}
+
+__device__ inline Seq planned_seq(const int32_t *plan, int64_t n_seqs, int s)
+{
+    Seq q;
+    q.row0 = uniform(plan[kPlanHead + kSeqRow0 * n_seqs + s]);
+    q.rows = uniform(plan[kPlanHead + kSeqRows * n_seqs + s]);
+    q.len = uniform(plan[kPlanHead + kSeqLen * n_seqs + s]);
+    q.pos0 = q.len - q.rows;
+    return q;
 }
 
 // Rows of sequence s that are no part of a partition of the batch's (2), a length that the table cannot hold (1).
@@ -152,7 +170,7 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
 #pragma unroll
     for (int k = 0; k < MOST; ++k) {
         const int s = lane * each + k;
-        q[k] = Seq{0, 0, 0};
+        q[k] = Seq{0, 0, 0, 0};
         if (k < each && s < n) {
             q[k] = seq_of(p.b, s);
             bad |= faults_of(p.b, s);
@@ -168,18 +186,18 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
         for (int k = 0; k < MOST; ++k) work += (float)tiles_of<kLong>(p, q[k]) * (float)reach_of<kLong>(p, q[k]);
         chunk = chunk_of(p, last_lane(wave_scan(work)));
     }
-    int own[MOST][kPlanArrays] = {}, sum[kPlanArrays] = {};
+    int own[MOST][kPlanSums] = {}, sum[kPlanSums] = {};
     if (!__any(bad & 2)) {                // rows that are no partition: no work at all
 #pragma unroll
         for (int k = 0; k < MOST; ++k) {
             if (k >= each) break;
             plan_entry(p, q[k], shift, chunk, own[k]);
 #pragma unroll
-            for (int a = 0; a < kPlanArrays; ++a) sum[a] += own[k][a];
+            for (int a = 0; a < kPlanSums; ++a) sum[a] += own[k][a];
         }
     }
 #pragma unroll
-    for (int a = 0; a < kPlanArrays; ++a) {
+    for (int a = 0; a < kPlanSums; ++a) {
         const int upto = wave_scan(sum[a]);
         int before = upto - sum[a];
         sum[a] = upto;                    // lane 63's is the total
@@ -190,6 +208,9 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
             before += own[k][a];
         }
     }
+#pragma unroll
+    for (int k = 0; k < MOST; ++k)
+        if (k < each && lane * each + k < n) store_seq(plan, n, lane * each + k, q[k]);
     if (lane == 63) plan_head(p, plan, shift, chunk, sum);
     if (bad && blockIdx.x == 0) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
 }
@@ -219,9 +240,9 @@ __device__ inline Place place_of(const AttnParams &p, const int32_t *plan, int u
     const int32_t *base = plan + kPlanHead + kBaseUnit * p.b.n_seqs;
     Place x;
     x.s = seq_at(p, base, unit);
-    q = seq_of(p.b, x.s);
-    x.units = units_of(reach_of<kShort>(p, q), plan[kUnitTokens]);
-    const int before = base[x.s];
+    q = planned_seq(plan, p.b.n_seqs, x.s);
+    x.units = units_of(reach_of<kShort>(p, q), uniform(plan[kUnitTokens]));
+    const int before = uniform(base[x.s]);
     const int pair = x.units == 1 ? unit - before : (unit - before) / x.units;
     x.start = before + pair * x.units;
     x.tile = pair / p.kv_div;

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
 {
     constexpr int WAVES = kPlanThreads / 64;
     __shared__ float s_work[WAVES], s_units[WAVES];
-    __shared__ int s_sum[kPlanArrays][WAVES];
+    __shared__ int s_sum[kPlanSums][WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = p.b.n_seqs;
     float work = 0.f, units = 0.f;
     unsigned bad = 0;
@@ -53,20 +53,24 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
     for (int w = 0; w < WAVES; ++w) work += s_work[w], units += s_units[w];
     const int shift = unit_shift_of(units);
     const int chunk = p.long_o ? chunk_of(p, work) : 1 << 30;
-    int base[kPlanArrays] = {};
+    int base[kPlanSums] = {};
     for (int s0 = 0; s0 < n; s0 += kPlanThreads) {
         const int s = s0 + tid;
-        int own[kPlanArrays] = {}, upto[kPlanArrays];
-        if (s < n && !no_rows) plan_entry(p, seq_of(p.b, s), shift, chunk, own);
+        int own[kPlanSums] = {}, upto[kPlanSums];
+        if (s < n) {
+            const Seq q = seq_of(p.b, s);
+            if (!no_rows) plan_entry(p, q, shift, chunk, own);
+            store_seq(p.plan, n, s, q);
+        }
         __syncthreads();                  // the round before has been read
 #pragma unroll
-        for (int a = 0; a < kPlanArrays; ++a) {
+        for (int a = 0; a < kPlanSums; ++a) {
             upto[a] = wave_scan(own[a]);
             if (lane == 63) s_sum[a][wave] = upto[a];
         }
         __syncthreads();
 #pragma unroll
-        for (int a = 0; a < kPlanArrays; ++a) {
+        for (int a = 0; a < kPlanSums; ++a) {
             int total = 0;
             for (int w = 0; w < WAVES; ++w) {
                 if (w < wave) upto[a] += s_sum[a][w];
@@ -118,22 +122,29 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
     const unsigned v_lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)s_v;
     float *s_o = reinterpret_cast<float *>(s_mem);
 
-    const int first = blockIdx.x * plan[kShare], end = min(first + plan[kShare], plan[kUnits]);
-    for (int u = first; u < end;) {
+    const int unit_shift = uniform(plan[kUnitTokens]), share = uniform(plan[kShare]);
+    const int first = blockIdx.x * share, end = min(first + share, uniform(plan[kUnits]));
+    if (first >= end) return;
+    const int place_mask = (1 << p.c.page_shift) - 1;
+
+    // A tile of the stretch, or the part of one: its rows, and its tokens [lo, hi).  Q's rows and the first page number are
+    // on their way before the tile before is written.
+    struct Part {
+        Seq q;
+        int s, head, tile, lo, hi, units;
+        bool whole, later;                // later: not the stretch's first tile
+    } part;
+    int see_lo[MT], see_hi[MT], all_lo, all_hi, page = 0;
+    bf16x8 qf[MT][KS];
+    const auto take = [&](int u) {
         Seq q;
         const Place pl = place_of(p, plan, u, q);
-        const int s = pl.s, head = pl.head, tile = pl.tile;
-        const int k0 = u - pl.start, k1 = min(pl.units, k0 + end - u);
-        const bool whole = k1 - k0 == pl.units;
-        const int64_t slot = 2 * blockIdx.x + (u != first);        // of a part: the workgroup's first tile, or its last
+        const int k0 = u - pl.start, k1 = min(pl.units, k0 + end - u), tile = pl.tile, head = pl.head;
         const Range rg = range_of<kShort>(p, q, tile);
-        const int lo = rg.lo + (k0 << plan[kUnitTokens]), hi = k1 == pl.units ? rg.hi : min(rg.hi, rg.lo + (k1 << plan[kUnitTokens]));
-        u += k1 - k0;
-        const int row0 = p.b.row_start[s];
-
+        const int lo = rg.lo + (k0 << unit_shift), hi = k1 == pl.units ? rg.hi : min(rg.hi, rg.lo + (k1 << unit_shift));
+        part = Part{q, pl.s, head, tile, lo, hi, k1 - k0, k1 - k0 == pl.units, u != first};
+        if (lo < hi) page = (p.b.table + (int64_t)pl.s * p.b.max_pages)[min(lo + wave * kBlock + (lane & 31), hi - 1) >> p.c.page_shift];
         // this lane's rows
-        int see_lo[MT], see_hi[MT];
-        bf16x8 qf[MT][KS];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const int r = tile * R + mt * 16 + col;
@@ -141,7 +152,7 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
             const bool real = r < q.rows * p.group;
             see_hi[mt] = !real ? 0 : p.causal ? min(hi, q.pos0 + i + 1) : hi;
             see_lo[mt] = p.window ? max(lo, q.pos0 + i - p.window + 1) : lo;
-            const uint16_t *from = p.q + (int64_t)(row0 + i) * p.ldq + (head * p.group + g) * D;
+            const uint16_t *from = p.q + (int64_t)(q.row0 + i) * p.ldq + (head * p.group + g) * D;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const int d = ks * 32 + grp * 8;
@@ -151,8 +162,13 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
             }
         }
         // tokens that every row of the tile sees; a block that goes beyond them has to be masked
-        const int all_lo = p.window ? q.pos0 + min(q.rows - 1, (tile * R + R - 1) / p.group_div) - p.window + 1 : lo;
-        const int all_hi = p.causal ? min(hi, q.pos0 + tile * R / p.group_div + 1) : hi;
+        all_lo = p.window ? q.pos0 + min(q.rows - 1, (tile * R + R - 1) / p.group_div) - p.window + 1 : lo;
+        all_hi = p.causal ? min(hi, q.pos0 + tile * R / p.group_div + 1) : hi;
+    };
+    take(first);
+    for (int u = first; u < end;) {
+        const int lo = part.lo, hi = part.hi, head = part.head;
+        u += part.units;
 
         f32x4 o[MT][DT];
         float m[MT], l[MT];
@@ -163,15 +179,12 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[mt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        const int32_t *table = p.b.table + (int64_t)s * p.b.max_pages;
-        const int place_mask = (1 << p.c.page_shift) - 1;
+        const int32_t *table = p.b.table + (int64_t)part.s * p.b.max_pages;
         const uint16_t *kbase = p.c.k + head * p.c.head_stride, *vbase = p.c.v + head * p.c.head_stride;
 
         // lane l looks up the page of the block's token l % 32, a block ahead; tokens past the range are read as
         // its last one and masked below
-        int page = 0;
         unsigned bad = 0;
-        if (lo < hi) page = table[min(lo + wave * kBlock + (lane & 31), hi - 1) >> p.c.page_shift];
         for (int j0 = lo + wave * kBlock; j0 < hi; j0 += kWaves * kBlock) {
             bad |= (unsigned)page >= (unsigned)p.c.n_pages;
             const int64_t at = (int64_t)min((unsigned)page, (unsigned)p.c.n_pages - 1u) * p.c.page_stride +
@@ -282,6 +295,9 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
             }
         }
         if (bad) atomicOr(p.b.status, LORA_STATUS_BAD_PAGE);
+        const Part done = part;
+        const int64_t slot = 2 * blockIdx.x + done.later;      // of a part's results: the stretch's first tile, or its last
+        if (u < end) take(u);
         // the four waves' parts of the range, 16 rows at a time
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -294,8 +310,8 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
             if (grp == 0) s_m[wave][col] = m[mt], s_l[wave][col] = sum_l;
             __syncthreads();
             const int row = threadIdx.x >> 4;
-            const int r = tile * R + mt * 16 + row;
-            if (r < q.rows * p.group) {
+            const int r = done.tile * R + mt * 16 + row;
+            if (r < done.q.rows * p.group) {
                 float top = s_m[0][row];
 #pragma unroll
                 for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][row]);
@@ -307,28 +323,28 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
                     total += f[w] * s_l[w][row];
                 }
                 const int i = r / p.group_div;
-                const int64_t t = row0 + i;
+                const int64_t t = done.q.row0 + i;
                 const int qh = head * p.group + r - i * p.group;
-                const int64_t part = slot * R + mt * 16 + row;
+                const int64_t at = slot * R + mt * 16 + row;
                 const float norm = total == 0.f ? 0.f : 1.f / total;
                 for (int d = (threadIdx.x & 15) * 4; d < D; d += 64) {
                     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int w = 0; w < kWaves; ++w)
                         sum += *reinterpret_cast<f32x4 *>(s_o + (w * 16 + row) * OS + d) * f[w];
-                    if (whole) {
+                    if (done.whole) {
                         u32x2 b;
                         b[0] = pack_bf16_rne(sum[0] * norm, sum[1] * norm);
                         b[1] = pack_bf16_rne(sum[2] * norm, sum[3] * norm);
                         *reinterpret_cast<u32x2 *>(p.out + t * p.ldo + qh * D + d) = b;
                     } else {
-                        st16f(p.part_o + part * D + d, sum);
+                        st16f(p.part_o + at * D + d, sum);
                     }
                 }
                 if ((threadIdx.x & 15) == 0) {
-                    if (!whole) {
-                        p.part_ml[part * 2] = top;
-                        p.part_ml[part * 2 + 1] = total;
+                    if (!done.whole) {
+                        p.part_ml[at * 2] = top;
+                        p.part_ml[at * 2 + 1] = total;
                     } else if (p.lse) {
                         p.lse[t * p.heads + qh] = total == 0.f ? -INFINITY : (ref * p.scale_log2 + __builtin_amdgcn_logf(total)) * kLn2;
                     }
@@ -409,19 +425,20 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         if (pl.start == cut || pl.start < b * share) return;       // between two tiles, or not the first end inside this one
         const int n = (pl.start + pl.units - 1) / share - b + 1;
         const int rows = min(1 << p.short_shift, q.rows * p.group - (pl.tile << p.short_shift));
-        for (int row = wave; row < rows; row += 4) {
+        for (int row = blockIdx.y * 4 + wave; row < rows; row += 4 * gridDim.y) {
             const int r = (pl.tile << p.short_shift) + row, i = r / p.group_div;
             // the part of workgroup b + c: its last tile if it starts before, else its first
             const auto part = [&](int c) { return ((int64_t)2 * (b + c) + (c == 0 && pl.start != b * share) << p.short_shift) + row; };
-            join_row<DP>(p, p.part_ml, p.part_o, n, part, p.b.row_start[pl.s] + i, pl.head * p.group + r - i * p.group);
+            join_row<DP>(p, p.part_ml, p.part_o, n, part, q.row0 + i, pl.head * p.group + r - i * p.group);
         }
         return;
     }
     const int32_t *base = plan + kPlanHead + kBaseJoin * p.b.n_seqs, *slots = plan + kPlanHead + kBaseSlot * p.b.n_seqs;
+    if (blockIdx.y) return;
     const int units = plan[kJoinUnits], chunk = plan[kChunk];
     for (int u = (blockIdx.x - p.join_blocks) * 4 + wave; u < units; u += (gridDim.x - p.join_blocks) * 4) {
         const int s = seq_at(p, base, u);
-        const Seq q = seq_of(p.b, s);
+        const Seq q = planned_seq(plan, p.b.n_seqs, s);
         const int left = u - base[s];
         const int i = left / p.heads_div, qh = left - i * p.heads;
         const int head = qh / p.group_div;
@@ -431,7 +448,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         if (cuts == 1) continue;
         const int slot = slots[s] + tile * splits_of(reach_of<kLong>(p, q), chunk) * p.c.n_heads + head;
         const auto part = [&](int c) { return (int64_t)(slot + c * p.c.n_heads) * kLongTile + r - tile * kLongTile; };
-        join_row<DP>(p, p.long_ml, p.long_o, cuts, part, p.b.row_start[s] + i, qh);
+        join_row<DP>(p, p.long_ml, p.long_o, cuts, part, q.row0 + i, qh);
     }
 }
 
@@ -526,7 +543,9 @@ hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s
     const unsigned join_long = k.has_long && reach > kLongMinSplit ? 1024 : 0;
     p.join_blocks = k.has_short && reach > 1 << kUnitShift ? (int)grid - 1 : 0;
     if (p.join_blocks + join_long > 0) {
-        const dim3 both(p.join_blocks + join_long), block(256);
+        // a wave per row of a tile, or per four rows where most sequences are likely to have one new row only
+        const unsigned rows = k.has_long ? 1 : (unsigned)std::min<int64_t>(1 << k.shift, (int64_t)(max_rows > 0 ? max_rows : p.b.n_rows) * p.group);
+        const dim3 both(p.join_blocks + join_long, (rows + 3) / 4), block(256);
         if (p.c.dim <= 64) hipLaunchKernelGGL(join_kernel<64>, both, block, 0, s, p);
         else if (p.c.dim <= 128) hipLaunchKernelGGL(join_kernel<128>, both, block, 0, s, p);
         else hipLaunchKernelGGL(join_kernel<256>, both, block, 0, s, p);

@@ -78,8 +78,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     // the cuts of a tile lie n_heads apart, tiles behind each other, those with the longest ranges first
     const int32_t *base = plan + kPlanHead + kBaseItem * p.b.n_seqs;
     const int seq = seq_at(p, base, n);
-    Seq q = seq_of(p.b, seq);
-    q.rows = uniform(q.rows), q.len = uniform(q.len), q.pos0 = q.len - q.rows;
+    const Seq q = planned_seq(plan, p.b.n_seqs, seq);
     const int left = uniform(n - base[seq]);
     const int pair = left / p.kv_div, head = left - pair * p.c.n_heads;
     const int chunk = uniform(plan[kChunk]);
@@ -99,7 +98,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     const int r = r0 + col;
     const int i = r / p.group_div, g = r - i * p.group;
     const bool real = r < n_rows;
-    const int64_t t = p.b.row_start[seq] + i;
+    const int64_t t = q.row0 + i;
     const int qh = head * p.group + g;
     const int see_hi = !real ? 0 : p.causal ? min(hi, q.pos0 + i + 1) : hi;
     const int see_lo = p.window ? max(lo, q.pos0 + i - p.window + 1) : lo;

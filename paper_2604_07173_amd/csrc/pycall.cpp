@@ -12,6 +12,7 @@
 #include <stdint.h>
 
 #include "../../include/lora.h"
+#include "../../include/lora_attn.h"
 
 namespace {
 
@@ -24,6 +25,11 @@ struct Library {
     decltype(&lora_moe_build_apply) moe_build_apply;
     decltype(&lora_moe_down_combine) moe_down_combine;
     decltype(&lora_pool_load_adapter_layer) load_adapter_layer;
+    decltype(&lora_rope_append) rope_append;
+    decltype(&lora_kv_attention) kv_attention;
+    decltype(&lora_kv_plan) kv_plan;
+    decltype(&lora_kv_compact) kv_compact;
+    decltype(&lora_kv_copy_pages) kv_copy_pages;
 } lib;
 
 // Python-side helpers, set by bind(): the slow but always right way to a stream's handle, and, once
@@ -100,19 +106,30 @@ struct Held {                                       // a reference for as long a
     ~Held() { Py_XDECREF(obj); }
 };
 
-// the lora_segments inside a Segments object (a ctypes structure, reached through the buffer protocol).
+// the C structure inside an object (a ctypes structure in its attribute `c`, reached through the buffer protocol).
 // `keep` holds the structure until the call is over: the object may hand out another one meanwhile
-bool segments_of(PyObject *v, lora_segments *&out, Held &keep)
+template <class T>
+bool structure_of(PyObject *v, T *&out, Held &keep, const char *what)
 {
     keep.obj = PyObject_GetAttr(v, s_c);
     if (!keep.obj) return false;
     Py_buffer view;
     if (PyObject_GetBuffer(keep.obj, &view, PyBUF_WRITABLE) != 0) return false;
-    out = static_cast<lora_segments *>(view.buf);
-    const bool fits = view.len >= (Py_ssize_t)sizeof(lora_segments);
+    out = static_cast<T *>(view.buf);
+    const bool fits = view.len >= (Py_ssize_t)sizeof(T);
     PyBuffer_Release(&view);
-    if (!fits) PyErr_SetString(PyExc_TypeError, "not a lora_segments structure");
+    if (!fits) PyErr_Format(PyExc_TypeError, "not a %s structure", what);
     return fits;
+}
+
+bool segments_of(PyObject *v, lora_segments *&out, Held &keep) { return structure_of(v, out, keep, "lora_segments"); }
+
+// the same, or None as a null pointer
+template <class T>
+bool structure_or_none(PyObject *v, T *&out, Held &keep, const char *what)
+{
+    out = nullptr;
+    return v == Py_None || structure_of(v, out, keep, what);
 }
 
 bool bytes_of(PyObject *tensor, size_t &out)
@@ -356,15 +373,113 @@ LORA_PY(load_adapter_layer)
     LORA_CALL(lib.load_adapter_layer(pool, adapter, layer, src, st));
 }
 
+// cache, layer, batch, rope, q, ldq, k, ldk, v, ldv, q_out, ldqo, n_heads, in_dtype, stream
+LORA_PY(rope_append)
+{
+    lora_kv_cache *c;
+    lora_kv_batch *b;
+    lora_rope *r;
+    Held c_ref, b_ref, r_ref;
+    int layer, heads, dt;
+    void *q, *k, *v, *qo, *st;
+    int64_t ldq, ldk, ldv, ldqo;
+    if (!n_args(n, 15) || !structure_or_none(a[0], c, c_ref, "lora_kv_cache") || !to_int(a[1], layer) ||
+        !structure_or_none(a[2], b, b_ref, "lora_kv_batch") || !structure_or_none(a[3], r, r_ref, "lora_rope") ||
+        !addr(a[4], q) || !to_i64(a[5], ldq) || !addr(a[6], k) || !to_i64(a[7], ldk) || !addr(a[8], v) || !to_i64(a[9], ldv) ||
+        !addr(a[10], qo) || !to_i64(a[11], ldqo) || !to_int(a[12], heads) || !to_int(a[13], dt) || !stream_of(a[14], st))
+        return nullptr;
+    LORA_CALL(lib.rope_append(c, layer, b, r, q, ldq, k, ldk, v, ldv, qo, ldqo, heads, dt, st));
+}
+
+// cache, layer, batch, q, ldq, n_heads, out, ldo, lse, scale, causal, window, ws, stream
+LORA_PY(kv_attention)
+{
+    lora_kv_cache *c;
+    lora_kv_batch *b;
+    Held c_ref, b_ref;
+    int layer, heads, window;
+    void *q, *o, *lse, *ws, *st;
+    int64_t ldq, ldo;
+    size_t bytes;
+    if (!n_args(n, 14) || !structure_or_none(a[0], c, c_ref, "lora_kv_cache") || !to_int(a[1], layer) ||
+        !structure_or_none(a[2], b, b_ref, "lora_kv_batch") || !addr(a[3], q) || !to_i64(a[4], ldq) || !to_int(a[5], heads) ||
+        !addr(a[6], o) || !to_i64(a[7], ldo) || !addr(a[8], lse) || !to_int(a[11], window) ||
+        !ws_of(a[12], Py_None, ws, bytes) || !stream_of(a[13], st))
+        return nullptr;
+    const double scale = PyFloat_AsDouble(a[9]);
+    if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    const int causal = PyObject_IsTrue(a[10]);
+    if (causal < 0) return nullptr;
+    LORA_CALL(lib.kv_attention(c, layer, b, q, ldq, heads, o, ldo, (float *)lse, (float)scale, causal, window, ws, bytes, st));
+}
+
+// cache, from, to, src, new_len, moves, stream
+LORA_PY(kv_plan)
+{
+    lora_kv_cache *c;
+    lora_kv_state *from, *to;
+    lora_kv_moves *m;
+    Held c_ref, f_ref, t_ref, m_ref;
+    void *src, *len, *st;
+    if (!n_args(n, 7) || !structure_or_none(a[0], c, c_ref, "lora_kv_cache") || !structure_or_none(a[1], from, f_ref, "lora_kv_state") ||
+        !structure_or_none(a[2], to, t_ref, "lora_kv_state") || !addr(a[3], src) || !addr(a[4], len) ||
+        !structure_or_none(a[5], m, m_ref, "lora_kv_moves") || !stream_of(a[6], st))
+        return nullptr;
+    LORA_CALL(lib.kv_plan(c, from, to, (const int32_t *)src, (const int32_t *)len, m, st));
+}
+
+// cache, from, to, moves, stream
+LORA_PY(kv_compact)
+{
+    lora_kv_cache *c;
+    lora_kv_state *from, *to;
+    lora_kv_moves *m;
+    Held c_ref, f_ref, t_ref, m_ref;
+    void *st;
+    if (!n_args(n, 5) || !structure_or_none(a[0], c, c_ref, "lora_kv_cache") || !structure_or_none(a[1], from, f_ref, "lora_kv_state") ||
+        !structure_or_none(a[2], to, t_ref, "lora_kv_state") || !structure_or_none(a[3], m, m_ref, "lora_kv_moves") ||
+        !stream_of(a[4], st))
+        return nullptr;
+    LORA_CALL(lib.kv_compact(c, from, to, m, st));
+}
+
+// cache, moves, max_moves, stream
+LORA_PY(kv_copy_pages)
+{
+    lora_kv_cache *c;
+    lora_kv_moves *m;
+    Held c_ref, m_ref;
+    int most;
+    void *st;
+    if (!n_args(n, 4) || !structure_or_none(a[0], c, c_ref, "lora_kv_cache") || !structure_or_none(a[1], m, m_ref, "lora_kv_moves") ||
+        !to_int(a[2], most) || !stream_of(a[3], st))
+        return nullptr;
+    LORA_CALL(lib.kv_copy_pages(c, m, most, st));
+}
+
+struct Wanted {
+    const char *name;
+    void **at;
+};
+
+bool address_of(PyObject *addresses, const char *name, void **at)
+{
+    PyObject *v = PyMapping_GetItemString(addresses, name);
+    if (!v) return false;
+    uint64_t p;
+    const bool ok = to_u64(v, p) && p;
+    Py_DECREF(v);
+    if (ok) *at = reinterpret_cast<void *>(p);
+    else if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "no address for %s", name);
+    return ok;
+}
+
 // bind(addresses, stream function): the library's functions by name, and the binding's own way from a
 // stream argument to its handle
 LORA_PY(bind)
 {
     if (!n_args(n, 2)) return nullptr;
-    struct {
-        const char *name;
-        void **at;
-    } const want[] = {
+    const Wanted want[] = {
         {"lora_build_segments", (void **)&lib.build_segments},
         {"lora_apply", (void **)&lib.apply},
         {"lora_apply_group", (void **)&lib.apply_group},
@@ -374,20 +489,24 @@ LORA_PY(bind)
         {"lora_moe_down_combine", (void **)&lib.moe_down_combine},
         {"lora_pool_load_adapter_layer", (void **)&lib.load_adapter_layer},
     };
-    for (const auto &w : want) {
-        PyObject *v = PyMapping_GetItemString(a[0], w.name);
-        if (!v) return nullptr;
-        uint64_t p;
-        const bool ok = to_u64(v, p) && p;
-        Py_DECREF(v);
-        if (!ok) {
-            if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "no address for %s", w.name);
-            return nullptr;
-        }
-        *w.at = reinterpret_cast<void *>(p);
-    }
+    for (const auto &w : want)
+        if (!address_of(a[0], w.name, w.at)) return nullptr;
     Py_INCREF(a[1]);
     Py_XSETREF(slow_stream, a[1]);
+    Py_RETURN_NONE;
+}
+
+// bind_kv(addresses): the functions of the paged cache
+LORA_PY(bind_kv)
+{
+    if (!n_args(n, 1)) return nullptr;
+    const Wanted want[] = {
+        {"lora_rope_append", (void **)&lib.rope_append}, {"lora_kv_attention", (void **)&lib.kv_attention},
+        {"lora_kv_plan", (void **)&lib.kv_plan},         {"lora_kv_compact", (void **)&lib.kv_compact},
+        {"lora_kv_copy_pages", (void **)&lib.kv_copy_pages},
+    };
+    for (const auto &w : want)
+        if (!address_of(a[0], w.name, w.at)) return nullptr;
     Py_RETURN_NONE;
 }
 
@@ -405,9 +524,10 @@ LORA_PY(use_current_stream)
 
 #define LORA_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
-    LORA_METHOD(bind), LORA_METHOD(use_current_stream), LORA_METHOD(build_segments), LORA_METHOD(apply),
+    LORA_METHOD(bind), LORA_METHOD(bind_kv), LORA_METHOD(use_current_stream), LORA_METHOD(build_segments), LORA_METHOD(apply),
     LORA_METHOD(apply_group), LORA_METHOD(build_apply_group), LORA_METHOD(moe_apply), LORA_METHOD(moe_build_apply),
-    LORA_METHOD(moe_down_combine), LORA_METHOD(load_adapter_layer), {nullptr, nullptr, 0, nullptr}};
+    LORA_METHOD(moe_down_combine), LORA_METHOD(load_adapter_layer), LORA_METHOD(rope_append),
+    LORA_METHOD(kv_attention), LORA_METHOD(kv_plan), LORA_METHOD(kv_compact), LORA_METHOD(kv_copy_pages), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
