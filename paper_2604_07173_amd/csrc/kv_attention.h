@@ -215,12 +215,15 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
     if (bad && blockIdx.x == 0) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
 }
 
-// The plan: made in s_plan by the workgroup's first wave, or what a launch before has left in the workspace.
+// The plan: made in s_plan by the workgroup's first wave, or what plan_kernel has left in the workspace.  The first workgroup
+// leaves its own there for the launch after.
 __device__ inline const int32_t *plan_of(const AttnParams &p, int32_t *s_plan)
 {
     if (p.b.n_seqs > kInlineSeqs) return p.plan;
     if (threadIdx.x < 64) make_plan(p, s_plan);
     __syncthreads();
+    if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < kPlanHead + kPlanArrays * p.b.n_seqs; i += blockDim.x) p.plan[i] = s_plan[i];
     return s_plan;
 }
 

@@ -414,11 +414,10 @@ __device__ inline void join_row(const AttnParams &p, const float *ml, const floa
 template <int DP>
 __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
 {
-    __shared__ int32_t s_plan[kInlineWords];
-    const int32_t *plan = plan_of(p, s_plan);
+    const int32_t *plan = p.plan;        // the kernels before have left it
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if ((int)blockIdx.x < p.join_blocks) {
-        const int share = plan[kShare], b = blockIdx.x, cut = (b + 1) * share;
+        const int share = uniform(plan[kShare]), b = blockIdx.x, cut = (b + 1) * share;
         if (cut >= plan[kUnits]) return;
         Seq q;
         const Place pl = place_of(p, plan, cut, q);
@@ -428,7 +427,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         for (int row = blockIdx.y * 4 + wave; row < rows; row += 4 * gridDim.y) {
             const int r = (pl.tile << p.short_shift) + row, i = r / p.group_div;
             // the part of workgroup b + c: its last tile if it starts before, else its first
-            const auto part = [&](int c) { return ((int64_t)2 * (b + c) + (c == 0 && pl.start != b * share) << p.short_shift) + row; };
+            const auto part = [&](int c) { return (((int64_t)2 * (b + c) + (c == 0 && pl.start != b * share)) << p.short_shift) + row; };
             join_row<DP>(p, p.part_ml, p.part_o, n, part, q.row0 + i, pl.head * p.group + r - i * p.group);
         }
         return;

@@ -267,6 +267,172 @@ __global__ __launch_bounds__(kThreads) void write_kernel(PlanParams p)
     if (threadIdx.x == 0) p.to_len[s] = r.len;
 }
 
+// ---- a plan in one launch, for caches of up to kSmallPages pages and tables of up to kSmallTable entries: one workgroup does
+// the steps above with its arrays in LDS.  Waves take slots in turn, with the table entries of eight slots on their way at a time. ----
+
+constexpr int kSmallPages = 8192, kSmallSeqs = 1024, kSmallTable = 1 << 14;
+constexpr int kDeep = 8;
+
+__global__ __launch_bounds__(kScanThreads) void small_plan_kernel(PlanParams p)
+{
+    __shared__ int s_ref[kSmallPages], s_grow[kSmallPages], s_low[kSmallPages], s_free[kSmallPages];
+    __shared__ int s_src[kSmallSeqs], s_keep[kSmallSeqs], s_len[kSmallSeqs];     // then: pages kept and asked for
+    constexpr int WAVES = kScanThreads / 64;
+    __shared__ int s_base[kSmallSeqs], s_cow[kSmallSeqs], s_sum[2][WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int i = tid; i < p.n_pages; i += kScanThreads) {
+        s_ref[i] = 0;
+        s_grow[i] = 0;
+        s_low[i] = INT_MAX;
+    }
+    unsigned bad = 0;
+    Slot own = {-1, 0, 0};
+    if (tid < p.n_seqs) {
+        own = slot_of(p, tid, bad);
+        s_src[tid] = max(own.src, 0);
+        s_keep[tid] = pages_of(own.keep, p.page_shift);
+        s_len[tid] = pages_of(own.len, p.page_shift);
+        s_cow[tid] = grows(p, own);
+    }
+    __syncthreads();
+    int most = 0;                         // of the slots' table entries in use, now and then
+    for (int s = lane; s < p.n_seqs; s += 64) most = max(most, max(s_keep[s], s_len[s]));
+#pragma unroll
+    for (int d = 32; d; d >>= 1) most = max(most, __shfl_xor(most, d));
+    for (int s0 = wave; s0 < p.n_seqs; s0 += WAVES * kDeep) {
+        int keep[kDeep];
+        const int32_t *row[kDeep];
+        const int mine = min(s0 + (lane & (kDeep - 1)) * WAVES, p.n_seqs - 1);       // lane k looks up slot k of the eight
+        const int my_keep = s_keep[mine], my_src = s_src[mine];
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            keep[k] = s0 + k * WAVES < p.n_seqs ? __builtin_amdgcn_readlane(my_keep, k) : 0;
+            row[k] = p.from_table + (int64_t)__builtin_amdgcn_readlane(my_src, k) * p.max_pages;
+        }
+        for (int i0 = 0; i0 < most; i0 += 64) {
+            const int i = i0 + lane;
+            int page[kDeep];
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) page[k] = row[k][min(i, p.max_pages - 1)];
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) {
+                if (i >= keep[k]) continue;
+                if ((unsigned)page[k] >= (unsigned)p.n_pages) {
+                    bad |= LORA_STATUS_BAD_PAGE;
+                    continue;
+                }
+                atomicAdd(&s_ref[page[k]], 1);
+                if (i == keep[k] - 1) {
+                    const int s = s0 + k * WAVES;
+                    s_base[s] = page[k];  // the last page, until the base takes its place
+                    if (s_cow[s]) {
+                        atomicAdd(&s_grow[page[k]], 1);
+                        atomicMin(&s_low[page[k]], s);
+                    }
+                }
+            }
+        }
+    }
+    __shared__ unsigned s_bad;
+    if (tid == 0) s_bad = 0;
+    __syncthreads();
+    if (bad) atomicOr(&s_bad, bad);
+    __syncthreads();
+    bad = s_bad;
+    int wanted = 0, copies = 0, n_free = 0;
+    if (!bad) {
+        int need = 0, cow = 0;
+        if (tid < p.n_seqs) {
+            if (s_cow[tid]) {
+                const int page = s_base[tid], ref = s_ref[page];
+                cow = ref > 1 && !(s_grow[page] == ref && s_low[page] == tid);
+            }
+            need = cow + s_len[tid] - s_keep[tid];
+        }
+        // a thread looks at eight pages that lie together
+        int free = 0;
+#pragma unroll
+        for (int k = 0; k < kSmallPages / kScanThreads; ++k) {
+            const int i = tid * (kSmallPages / kScanThreads) + k;
+            free += i < p.n_pages && s_ref[i] == 0;
+        }
+        // pages asked for and copies in one number: no more than kSmallTable + kSmallSeqs and kSmallSeqs in all
+        const int both = need << 11 | cow, upto = wave_scan(both), upto_free = wave_scan(free);
+        static_assert(((int64_t)kSmallTable + kSmallSeqs) << 11 < INT_MAX && kSmallSeqs < 1 << 11, "both fit");
+        if (lane == 63) s_sum[0][wave] = upto, s_sum[1][wave] = upto_free;
+        __syncthreads();
+        int before = upto - both, rank = upto_free - free, total = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < wave) before += s_sum[0][w], rank += s_sum[1][w];
+            total += s_sum[0][w];
+            n_free += s_sum[1][w];
+        }
+        wanted = total >> 11;
+        copies = total & 2047;
+        if (tid < p.n_seqs) {
+            s_base[tid] = before >> 11;
+            s_cow[tid] = cow ? before & 2047 : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kSmallPages / kScanThreads; ++k) {
+            const int i = tid * (kSmallPages / kScanThreads) + k;
+            if (i >= p.n_pages || s_ref[i]) continue;
+            s_free[rank] = i;
+            s_low[i] = rank++;            // of a free page
+        }
+        __syncthreads();
+    }
+    const bool go = !bad && wanted <= n_free;
+    if (p.to_ref)
+        for (int i = tid; i < p.n_pages; i += kScanThreads) {
+            if (go) p.to_ref[i] = s_ref[i] ? s_ref[i] - copies_of(s_ref[i], s_grow[i]) : s_low[i] < wanted;
+            else if (p.from_ref) p.to_ref[i] = p.from_ref[i];
+        }
+    if (tid == 0) {
+        const int used = p.n_pages - n_free + (go ? wanted : 0);
+        p.counts[0] = go ? used : 0;
+        p.counts[1] = go ? copies : 0;
+        p.counts[2] = go ? p.n_pages - used : 0;
+        p.counts[3] = bad ? 0 : wanted;
+        if (!go) atomicOr(p.status, bad ? bad : (unsigned)LORA_STATUS_NO_PAGES);
+    }
+    if (tid < p.n_seqs) p.to_len[tid] = go ? own.len : p.from_len[tid];
+    for (int s0 = wave; s0 < p.n_seqs; s0 += WAVES * kDeep) {
+        int keep[kDeep], now[kDeep], base[kDeep], move[kDeep];
+        const int32_t *row[kDeep];
+        const int mine = min(s0 + (lane & (kDeep - 1)) * WAVES, p.n_seqs - 1);
+        const int my_keep = go ? s_keep[mine] : p.max_pages, my_len = go ? s_len[mine] : p.max_pages, my_base = go ? s_base[mine] : 0;
+        const int my_move = go ? s_cow[mine] : -1, my_src = go ? s_src[mine] : mine;
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) {
+            keep[k] = __builtin_amdgcn_readlane(my_keep, k);
+            now[k] = __builtin_amdgcn_readlane(my_len, k);
+            base[k] = __builtin_amdgcn_readlane(my_base, k);
+            move[k] = __builtin_amdgcn_readlane(my_move, k);
+            row[k] = p.from_table + (int64_t)__builtin_amdgcn_readlane(my_src, k) * p.max_pages;
+        }
+        for (int i0 = 0; i0 < p.max_pages; i0 += 64) {
+            const int i = i0 + lane;
+            int page[kDeep];
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) page[k] = row[k][min(i, p.max_pages - 1)];
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) {
+                const int s = s0 + k * WAVES;
+                if (s >= p.n_seqs || i >= p.max_pages) continue;
+                if (move[k] >= 0 && i == keep[k] - 1) {
+                    p.pairs[2 * move[k]] = page[k];
+                    p.pairs[2 * move[k] + 1] = page[k] = s_free[base[k]];
+                } else if (i >= keep[k]) {
+                    page[k] = i < now[k] ? s_free[base[k] + (move[k] >= 0) + i - keep[k]] : -1;
+                }
+                p.to_table[(int64_t)s * p.max_pages + i] = page[k];
+            }
+        }
+    }
+}
+
 // ---- compaction: pages in use with numbers from the number of pages in use on move to the free numbers below.
 // The r-th such page, in order, goes to the r-th free number.  chunk holds free pages per chunk, as above. ----
 
@@ -385,6 +551,10 @@ size_t plan_ws_bytes(int n_pages, int n_seqs)
 
 hipError_t launch_plan(const PlanParams &p, hipStream_t s)
 {
+    if (p.n_pages <= kSmallPages && p.n_seqs <= kSmallSeqs && (int64_t)p.n_seqs * p.max_pages <= kSmallTable) {
+        hipLaunchKernelGGL(small_plan_kernel, dim3(1), dim3(kScanThreads), 0, s, p);
+        return hipGetLastError();
+    }
     const int chunks = chunks_of(p.n_pages);
     hipLaunchKernelGGL(clear_kernel, dim3((std::max(p.n_pages, (int)kHeadWords) + kThreads - 1) / kThreads), dim3(kThreads), 0, s, p);
     hipLaunchKernelGGL(count_kernel, dim3(p.n_seqs), dim3(kThreads), 0, s, p);

@@ -105,7 +105,7 @@ def check(books, state, moves, pairs, wanted):
 
 
 @pytest.mark.parametrize("page", [1, 4, 16])
-@pytest.mark.parametrize("n_slots,n_pages", [(1, 5), (7, 40), (64, 700), (65, 3000), (1500, 5000)])
+@pytest.mark.parametrize("n_slots,n_pages", [(1, 5), (7, 40), (64, 700), (65, 3000), (1000, 8192), (1500, 5000), (50, 9000), (700, 20000)])
 def test_a_run_of_plans(page, n_slots, n_pages):
     """Growth, ends, falls back and forks at random, step after step, with a compaction now and then."""
     rng = np.random.default_rng(n_slots + page)
