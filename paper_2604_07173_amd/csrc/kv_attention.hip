@@ -190,11 +190,14 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
             const int64_t at = (int64_t)min((unsigned)page, (unsigned)p.c.n_pages - 1u) * p.c.page_stride +
                                (int64_t)(min(j0 + (lane & 31), hi - 1) & place_mask) * p.c.token_stride;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the block before has been read
+            // V is streamed where a tile holds all rows of most sequences, so that nobody reads it again (decode of 256 users
+            // 231 -> 214 us, of three long contexts 187 -> 169; K as well 217 and 170: its lines are fetched in two halves);
+            // with two tiles of a sequence it costs (drafted rows 38.1 -> 39.1)
 #pragma unroll
             for (int k = 0; k < VL; ++k) {
                 const int row = k * RPL + lane / CH, d = swizzled<DP>(row, lane % CH) * 8;
                 const int64_t from = __shfl(at, row) + d;
-                load_to_lds<false>(FULL || d < D ? (const void *)(vbase + from) : (const void *)zeros, v_lds + k * 1024);
+                load_to_lds<MT == 1>(FULL || d < D ? (const void *)(vbase + from) : (const void *)zeros, v_lds + k * 1024);
             }
             u32x4 kx[2][KS];
 #pragma unroll
