@@ -18,7 +18,10 @@ constexpr int kLongTile = 128;           // rows
 constexpr int kUnitShift = 7;            // a unit is 128 tokens: a step of a workgroup's four waves
 constexpr float kMostUnits = 1 << 29;    // on the line; units are doubled until there are no more
 constexpr int kMostBlocks = 768;         // workgroups of short tiles: three on every CU
-constexpr int kLongTarget = 512;         // items of long tiles that fill the chip
+// Items of long tiles that fill the chip: one on every CU.  Two fit, but the second adds less than writing and joining the parts
+// of more cuts costs (4 chunks of 64 rows over 2000 tokens, 32 / 8 heads: 34.5 us, with twice the items 37.4; 2 chunks of 512 rows
+// over 1500: 56 and 74; 8 of 128 over 500: 27 and 50; one of 200 over 8000: 58.7 and 55.8)
+constexpr int kLongTarget = 256;
 constexpr int kLongMinSplit = 512;       // tokens of a cut range at least
 constexpr int kShortLimit = 64;          // rows x group up to which a sequence goes in short tiles
 constexpr float kLn2 = 0.6931471805599453f;
