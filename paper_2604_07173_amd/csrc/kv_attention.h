@@ -23,7 +23,11 @@ constexpr int kMostBlocks = 768;         // workgroups of short tiles: three on 
 // over 1500: 56 and 74; 8 of 128 over 500: 27 and 50; one of 200 over 8000: 58.7 and 55.8)
 constexpr int kLongTarget = 256;
 constexpr int kLongMinSplit = 512;       // tokens of a cut range at least
-constexpr int kShortLimit = 64;          // rows x group up to which a sequence goes in short tiles
+// rows x group up to which a sequence goes in short tiles, where all have as many and where they differ.  Long tiles are faster
+// from 33 on (32 sequences of 12 rows and 4 heads each over 1500 tokens 64.7 / 49.3 us in short / long tiles), but a batch of both
+// takes two kernels, one after the other (48 uneven sequences of up to 13 rows, 5 x 4 heads of 80: 38.2 us in short tiles, 49.8
+// in both)
+constexpr int kShortEqual = 32, kShortLimit = 64;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kInlineSeqs = 256;         // sequences up to which every workgroup makes the plan for itself, in LDS: one launch less
 

@@ -470,8 +470,9 @@ Kinds kinds_of(int n_seqs, int n_rows, int max_rows, int heads, int kv_heads, in
     const int64_t group = heads / kv_heads;
     const int64_t most = max_rows > 0 ? std::min(max_rows, n_rows) : n_rows;
     Kinds k;
-    k.has_long = most * group > kShortLimit;
-    k.has_short = !k.has_long || !(max_rows > 0 && (int64_t)max_rows * n_seqs == n_rows);
+    const bool equal = max_rows > 0 && (int64_t)max_rows * n_seqs == n_rows;
+    k.has_long = most * group > (equal ? kShortEqual : kShortLimit);
+    k.has_short = !k.has_long || !equal;
     // a sequence with more rows than the host thought still has to go somewhere
     k.limit = !k.has_long ? INT_MAX : !k.has_short ? 0 : kShortLimit;
     k.shift = !k.has_long && most * group > 16 && dim <= 128 ? 5 : 4;

@@ -148,6 +148,9 @@ def test_unknown_or_wrong_longest_chunk():
     """max_rows decides which kernels run, never what comes out."""
     for given in (0, 1, 7, 1000):
         run(KvCase([3, 0, 50, 1, 133], [30, 20, 77, 5, 140], 4, 2, 128, seed=11, max_rows=given))
+    # as if all sequences had as many
+    run(KvCase([1, 0, 9, 2, 3], [30, 20, 77, 5, 140], 4, 2, 128, seed=11, max_rows=3))
+    run(KvCase([40, 0, 50, 10, 0], [40, 20, 77, 15, 140], 4, 2, 128, seed=11, max_rows=20))
 
 
 def test_strides_and_layers():
