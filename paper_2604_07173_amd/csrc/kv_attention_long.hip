@@ -11,7 +11,7 @@
 //
 // Measured, 32 / 8 heads of 128: 8 prompts of 2048 rows 365 us, 750 TFLOP/s of the visible pairs; 1984 rows over 18000 tokens 626 us,
 // 870 TFLOP/s, where the clock falls to 1.93 GHz (a large library product reaches 1369 TFLOP/s on this card).  Of the SIMDs' time
-// there the products take 44 % and vector instructions 54 %, LDS is busy for 66 % (K 8 cycles a read
+// there the products take 43 % and vector instructions 52 %, LDS is busy for 64 % (K 8 cycles a read
 // of 1 KiB, V 8 cycles a transposed read of 512 bytes).
 // Tried and left out, as slower: 64 rows per wave, which halves the LDS reads but needs 512 registers, between whose two
 // halves the compiler moves the outputs at every branch (2.2 ms; 377 us with 32); a step's scores formed while the weights of
