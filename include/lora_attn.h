@@ -55,7 +55,8 @@ typedef struct lora_kv_cache {
  * its n stands at position seq_len[s] - n + i.  Token p of sequence s is in page
  * table[s * max_pages + p / page_size], at place p % page_size.  A sequence may have no rows.
  * row_start[0] = 0, row_start does not fall, row_start[n_seqs] = n_rows; if not, attention raises
- * LORA_STATUS_BAD_LENGTH and writes nothing.
+ * LORA_STATUS_BAD_LENGTH and writes nothing, and lora_rope_append raises it for rows of no sequence and
+ * leaves them out of the cache.
  */
 typedef struct lora_kv_batch {
     int32_t n_seqs;             /* >= 1 */
@@ -121,8 +122,8 @@ typedef struct lora_rope {
  * v both NULL: only q.  rope NULL: nothing is rotated.  q_out may be q itself (bf16, ldqo ==
  * ldq); other overlaps of inputs and outputs are not allowed.  Two sequences that write to one
  * page at the same place race: lora_kv_plan gives every sequence a page of its own to write to.
- * A row whose place is outside the table or whose page is outside the cache is not written
- * (LORA_STATUS_BAD_LENGTH, LORA_STATUS_BAD_PAGE), its q is.  One launch.
+ * A row of no sequence, or whose place is outside the table, or whose page is outside the cache is not
+ * written (LORA_STATUS_BAD_LENGTH twice, LORA_STATUS_BAD_PAGE), its q is.  One launch.
  */
 int lora_rope_append(const lora_kv_cache *cache, int layer, const lora_kv_batch *batch,
                      const lora_rope *rope, const void *q, int64_t ldq, const void *k, int64_t ldk,

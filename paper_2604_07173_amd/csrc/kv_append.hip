@@ -68,10 +68,12 @@ __global__ __launch_bounds__(256) void append_kernel(AppendParams p)
     int pos = 0;
     if (p.kv_heads || !p.b.position) {
         const int s = wave_find(p.b.row_start, p.b.n_seqs, t);
-        pos = p.b.seq_len[s] - p.b.row_start[s + 1] + t;
+        const int start = p.b.row_start[s], end = p.b.row_start[s + 1];
+        pos = p.b.seq_len[s] - end + t;
         if (p.kv_heads && tid == 0) {
             int64_t at = -1;
-            if (pos < 0 || pos >= p.b.tokens_max) {
+            // a row of no sequence would stand where tokens of this one are, or where another one's may be
+            if (t < start || t >= end || pos < 0 || pos >= p.b.tokens_max) {
                 atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
             } else {
                 const int page = p.b.table[(int64_t)s * p.b.max_pages + (pos >> p.c.page_shift)];
