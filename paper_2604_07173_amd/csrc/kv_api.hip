@@ -6,6 +6,7 @@
 #include <cmath>
 
 #include "kv_internal.h"
+#include "kv_layout.h"
 
 using namespace lora;
 
@@ -324,23 +325,12 @@ int lora_kv_copy_pages(const lora_kv_cache *cache, const lora_kv_moves *moves, i
     p.counts = moves->counts;
     p.layer_stride = cache->layer_stride;
     p.page_stride = cache->page_stride;
-    // a page as runs that lie together: of heads and tokens the one with the smaller stride is inside
-    const bool token_in = cache->token_stride <= cache->head_stride;
-    p.run = cache->head_dim;
-    p.inner = token_in ? cache->page_size : cache->n_heads;
-    p.outer = token_in ? cache->n_heads : cache->page_size;
-    p.inner_stride = token_in ? cache->token_stride : cache->head_stride;
-    p.outer_stride = token_in ? cache->head_stride : cache->token_stride;
-    if (p.inner_stride == p.run || p.inner == 1) {
-        p.run *= p.inner;
-        p.inner = p.outer;
-        p.inner_stride = p.outer_stride;
-        p.outer = 1;
-        if (p.inner_stride == p.run) {
-            p.run *= p.inner;
-            p.inner = 1;
-        }
-    }
+    const PageRuns r = page_runs(*cache);
+    p.run = r.run;
+    p.inner = r.inner;
+    p.outer = r.outer;
+    p.inner_stride = r.inner_stride;
+    p.outer_stride = r.outer_stride;
     p.run_vecs = fast_div(p.run / 8);
     p.inner_div = fast_div(p.inner);
     p.n_layers = cache->n_layers;
