@@ -27,8 +27,14 @@ int log2_of(int n)
     return s;
 }
 
-// Elements from the first to the last of n things that lie `stride` apart and are `each` long.
-int64_t span(int64_t n, int64_t stride, int64_t each) { return (n - 1) * stride + each; }
+constexpr int64_t kMaxExtent = (int64_t)1 << 61;      // elements: their bytes are counted in 63 bits too
+
+// Elements from the first to the last of n things that lie `stride` apart and are `each` long, 0 if beyond kMaxExtent.
+int64_t span(int64_t n, int64_t stride, int64_t each)
+{
+    int64_t far;
+    return __builtin_mul_overflow(n - 1, stride, &far) || far > kMaxExtent - each ? 0 : far + each;
+}
 
 int check_cache(const lora_kv_cache *c)
 {
@@ -47,14 +53,18 @@ int check_cache(const lora_kv_cache *c)
     const int64_t s_in = token_in ? c->token_stride : c->head_stride, s_out = token_in ? c->head_stride : c->token_stride;
     if (n_in > 1 && s_in < c->head_dim) return LORA_ERR_BAD_SHAPE;
     const int64_t inner = span(n_in, s_in, c->head_dim);
+    if (!inner) return LORA_ERR_TOO_LARGE;
     if (n_out > 1 && s_out < inner) return LORA_ERR_BAD_SHAPE;
     const int64_t page = span(n_out, s_out, inner);
+    if (!page) return LORA_ERR_TOO_LARGE;
     const bool page_in = c->n_layers == 1 || (c->n_pages > 1 && c->page_stride <= c->layer_stride);
     const int64_t m_in = page_in ? c->n_pages : c->n_layers, m_out = page_in ? c->n_layers : c->n_pages;
     const int64_t t_in = page_in ? c->page_stride : c->layer_stride, t_out = page_in ? c->layer_stride : c->page_stride;
     if (m_in > 1 && t_in < page) return LORA_ERR_BAD_SHAPE;
-    if (m_out > 1 && t_out < span(m_in, t_in, page)) return LORA_ERR_BAD_SHAPE;
-    return LORA_OK;
+    const int64_t pages = span(m_in, t_in, page);
+    if (!pages) return LORA_ERR_TOO_LARGE;
+    if (m_out > 1 && t_out < pages) return LORA_ERR_BAD_SHAPE;
+    return span(m_out, t_out, pages) ? LORA_OK : LORA_ERR_TOO_LARGE;
 }
 
 // with_cache: the call uses the tables

@@ -1,0 +1,36 @@
+"""Caches whose last element lies further out than 64 bits of elements can say are refused, however the strides wrap."""
+import ctypes as C
+
+import pytest
+
+import paper_2604_07173_amd as L
+from paper_2604_07173_amd import binding as B
+
+A = 0x10000
+OK, LARGE = 0, -8
+
+
+def status(**kw):
+    d = dict(k=A, v=A, n_layers=2, n_pages=10, n_heads=4, page_size=16, head_dim=64, layer_stride=40960, page_stride=4096,
+             head_stride=1024, token_stride=64)
+    d.update(kw)
+    return L.load_library().lora_kv_copy_pages(C.byref(B._KvCache(**d)), C.byref(B._KvMoves(1, 0, A, A, A, A, 1 << 20)), 0, None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(n_pages=(1 << 16) + 1, page_stride=1 << 48),                        # 2^64: wraps to the page alone
+    dict(n_pages=(1 << 20) + 1, page_stride=1 << 44),
+    dict(n_pages=(1 << 30) + 5, page_stride=1 << 40, layer_stride=1 << 44),
+    dict(n_heads=32767, head_stride=1 << 48, page_stride=1 << 48, n_pages=1),
+    dict(n_layers=16384, layer_stride=1 << 48),                              # elements fit, bytes do not
+    dict(n_pages=1 << 20, page_stride=1 << 42, n_layers=1),
+])
+def test_extents_that_do_not_fit(change):
+    assert status(**change) == LARGE
+
+
+def test_large_extents_that_fit():
+    assert status() == OK
+    assert status(n_pages=1 << 24, page_stride=1 << 20, layer_stride=1 << 45) == OK
+    assert status(n_layers=256, layer_stride=1 << 48) == OK
+    assert status(n_pages=(1 << 31) - 1024, n_layers=1) == OK
