@@ -3,6 +3,7 @@
 #include <limits.h>
 #include <string.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "kv_internal.h"
@@ -47,24 +48,18 @@ int check_cache(const lora_kv_cache *c)
     const int64_t strides[4] = {c->layer_stride, c->page_stride, c->head_stride, c->token_stride};
     for (int64_t s : strides)
         if (s < 0 || s % 8 || s > ((int64_t)1 << 48)) return LORA_ERR_BAD_SHAPE;
-    // of heads and tokens, of a page and the layers, the one with the smaller stride lies inside the other
-    const bool token_in = c->n_heads == 1 || (c->page_size > 1 && c->token_stride <= c->head_stride);
-    const int64_t n_in = token_in ? c->page_size : c->n_heads, n_out = token_in ? c->n_heads : c->page_size;
-    const int64_t s_in = token_in ? c->token_stride : c->head_stride, s_out = token_in ? c->head_stride : c->token_stride;
-    if (n_in > 1 && s_in < c->head_dim) return LORA_ERR_BAD_SHAPE;
-    const int64_t inner = span(n_in, s_in, c->head_dim);
-    if (!inner) return LORA_ERR_TOO_LARGE;
-    if (n_out > 1 && s_out < inner) return LORA_ERR_BAD_SHAPE;
-    const int64_t page = span(n_out, s_out, inner);
-    if (!page) return LORA_ERR_TOO_LARGE;
-    const bool page_in = c->n_layers == 1 || (c->n_pages > 1 && c->page_stride <= c->layer_stride);
-    const int64_t m_in = page_in ? c->n_pages : c->n_layers, m_out = page_in ? c->n_layers : c->n_pages;
-    const int64_t t_in = page_in ? c->page_stride : c->layer_stride, t_out = page_in ? c->layer_stride : c->page_stride;
-    if (m_in > 1 && t_in < page) return LORA_ERR_BAD_SHAPE;
-    const int64_t pages = span(m_in, t_in, page);
-    if (!pages) return LORA_ERR_TOO_LARGE;
-    if (m_out > 1 && t_out < pages) return LORA_ERR_BAD_SHAPE;
-    return span(m_out, t_out, pages) ? LORA_OK : LORA_ERR_TOO_LARGE;
+    // each, in the order of the strides, begins beyond all that those with smaller ones span
+    struct {
+        int64_t n, stride;
+    } dims[4] = {{c->n_layers, c->layer_stride}, {c->n_pages, c->page_stride}, {c->n_heads, c->head_stride}, {c->page_size, c->token_stride}};
+    std::sort(dims, dims + 4, [](const auto &a, const auto &b) { return a.stride < b.stride; });
+    int64_t extent = c->head_dim;
+    for (const auto &d : dims) {
+        if (d.n == 1) continue;
+        if (d.stride < extent) return LORA_ERR_BAD_SHAPE;
+        if (!(extent = span(d.n, d.stride, extent))) return LORA_ERR_TOO_LARGE;
+    }
+    return LORA_OK;
 }
 
 // with_cache: the call uses the tables

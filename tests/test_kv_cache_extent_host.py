@@ -1,5 +1,7 @@
-"""Caches whose last element lies further out than 64 bits of elements can say are refused, however the strides wrap."""
+"""Layouts of caches that the calls take and refuse, and caches whose last element lies further out than 64 bits of elements can say, which
+are refused however the strides wrap."""
 import ctypes as C
+import itertools
 
 import pytest
 
@@ -7,7 +9,7 @@ import paper_2604_07173_amd as L
 from paper_2604_07173_amd import binding as B
 
 A = 0x10000
-OK, LARGE = 0, -8
+OK, SHAPE, LARGE = 0, -2, -8
 
 
 def status(**kw):
@@ -34,3 +36,19 @@ def test_large_extents_that_fit():
     assert status(n_pages=1 << 24, page_stride=1 << 20, layer_stride=1 << 45) == OK
     assert status(n_layers=256, layer_stride=1 << 48) == OK
     assert status(n_pages=(1 << 31) - 1024, n_layers=1) == OK
+
+
+DIMS = dict(l=("n_layers", "layer_stride", 2), p=("n_pages", "page_stride", 10), h=("n_heads", "head_stride", 4),
+            t=("page_size", "token_stride", 16))
+
+
+@pytest.mark.parametrize("order", list(itertools.permutations("lpht")), ids="".join)
+def test_every_order_is_taken_and_none_that_overlaps(order):
+    strides, each = {}, 64
+    for d in reversed(order):
+        strides[DIMS[d][1]] = each
+        each *= DIMS[d][2]
+    assert status(**strides) == OK
+    for d in order:                                # a stride eight less: one thing begins inside another one
+        assert status(**dict(strides, **{DIMS[d][1]: strides[DIMS[d][1]] - 8})) == SHAPE
+        assert status(**dict(strides, **{DIMS[d][0]: 1, DIMS[d][1]: 0})) == OK       # of which there is one: any stride
