@@ -22,6 +22,7 @@ extern "C" {
 enum {
     LORA_KV_MAX_HEAD_DIM = 256,
     LORA_KV_MAX_PAGE = 1024,      /* tokens of a page */
+    LORA_KV_MAX_PAGES = 0x7FFFFC00,      /* pages of a cache: chunks of 1024 are numbered in 32 bits */
     LORA_KV_MAX_GROUP = 64        /* query heads that share a key/value head */
 };
 
@@ -39,10 +40,11 @@ enum {
  * (layer, page, head, token, d) of K is at k + layer * layer_stride + page * page_stride +
  * head * head_stride + token * token_stride + d, of V likewise; strides are in elements and
  * multiples of 8, and layers, pages, heads and tokens may lie in any order in which each begins beyond
- * what those with smaller strides span (LORA_ERR_BAD_SHAPE); of what there is one, any
- * multiple of 8 will do.  The last element is less than 2^61 elements from the first
- * (LORA_ERR_TOO_LARGE).  k and v are 16-byte aligned device memory.  page_size: a power of two, 1 .. LORA_KV_MAX_PAGE.  head_dim: a
- * multiple of 8, 8 .. LORA_KV_MAX_HEAD_DIM.  All layers share the tables.
+ * what those with smaller strides span (LORA_ERR_BAD_SHAPE); of what there is one, any multiple of 8
+ * will do.  The last element is less than 2^61 elements from the first (LORA_ERR_TOO_LARGE).  k and v
+ * are 16-byte aligned device memory.  n_pages: 1 .. LORA_KV_MAX_PAGES.  page_size: a power of two,
+ * 1 .. LORA_KV_MAX_PAGE.  head_dim: a multiple of 8, 8 .. LORA_KV_MAX_HEAD_DIM.  All layers share the
+ * tables.
  * ------------------------------------------------------------------------------------ */
 typedef struct lora_kv_cache {
     void *k, *v;

@@ -21,7 +21,7 @@ from .binding import (  # noqa: F401
     lora_kv_attention_ws_bytes, lora_kv_attention, lora_kv_moves_ws_bytes, lora_kv_plan, lora_kv_compact, lora_kv_copy_pages,
     LORA_STATUS_BAD_PAGE, LORA_STATUS_BAD_LENGTH, LORA_STATUS_BAD_SEQ, LORA_STATUS_NO_PAGES, LORA_ROPE_HALF,
     LORA_ROPE_INTERLEAVED, LORA_ROPE_PLAIN, LORA_ROPE_LINEAR, LORA_ROPE_BASE, LORA_ROPE_PARTS, LORA_KV_MAX_HEAD_DIM,
-    LORA_KV_MAX_PAGE, LORA_KV_MAX_GROUP,
+    LORA_KV_MAX_PAGE, LORA_KV_MAX_PAGES, LORA_KV_MAX_GROUP,
     EXPORTED_SYMBOLS,
     ProvisionError, lora_provision_iar, lora_provision_min_cache, lora_provision_memory_bytes,
 )

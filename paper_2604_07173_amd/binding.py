@@ -20,7 +20,7 @@ LORA_STATIC_WS_BYTES = 16 << 20
 LORA_STATUS_BAD_PAGE, LORA_STATUS_BAD_LENGTH, LORA_STATUS_BAD_SEQ, LORA_STATUS_NO_PAGES = 4, 8, 16, 32
 LORA_ROPE_HALF, LORA_ROPE_INTERLEAVED = 0, 1
 LORA_ROPE_PLAIN, LORA_ROPE_LINEAR, LORA_ROPE_BASE, LORA_ROPE_PARTS = 0, 1, 2, 3
-LORA_KV_MAX_HEAD_DIM, LORA_KV_MAX_PAGE, LORA_KV_MAX_GROUP = 256, 1024, 64
+LORA_KV_MAX_HEAD_DIM, LORA_KV_MAX_PAGE, LORA_KV_MAX_PAGES, LORA_KV_MAX_GROUP = 256, 1024, 0x7FFFFC00, 64
 
 EXPORTED_SYMBOLS = [
     "lora_strerror", "lora_last_hip_error", "lora_pool_bytes", "lora_register_pool",

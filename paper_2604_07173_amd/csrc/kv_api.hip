@@ -42,7 +42,7 @@ int check_cache(const lora_kv_cache *c)
     if (!c || !c->k || !c->v) return LORA_ERR_INVALID_ARG;
     if (!aligned(c->k, 16) || !aligned(c->v, 16)) return LORA_ERR_MISALIGNED;
     if (c->n_layers < 1 || c->n_pages < 1 || c->n_heads < 1) return LORA_ERR_INVALID_ARG;
-    if (c->n_layers > 16384 || c->n_heads > 32768) return LORA_ERR_TOO_LARGE;
+    if (c->n_layers > 16384 || c->n_heads > 32768 || c->n_pages > LORA_KV_MAX_PAGES) return LORA_ERR_TOO_LARGE;
     if (c->page_size < 1 || c->page_size > LORA_KV_MAX_PAGE || (c->page_size & (c->page_size - 1))) return LORA_ERR_BAD_SHAPE;
     if (c->head_dim < 8 || c->head_dim > LORA_KV_MAX_HEAD_DIM || c->head_dim % 8) return LORA_ERR_BAD_SHAPE;
     const int64_t strides[4] = {c->layer_stride, c->page_stride, c->head_stride, c->token_stride};
@@ -288,7 +288,7 @@ int lora_kv_attention(const lora_kv_cache *cache, int layer, const lora_kv_batch
 
 size_t lora_kv_moves_ws_bytes(int n_pages, int n_seqs)
 {
-    if (n_pages < 1 || n_seqs < 1 || n_seqs > LORA_MAX_ROWS_LONG) return 0;
+    if (n_pages < 1 || n_pages > LORA_KV_MAX_PAGES || n_seqs < 1 || n_seqs > LORA_MAX_ROWS_LONG) return 0;
     return plan_ws_bytes(n_pages, n_seqs);
 }
 

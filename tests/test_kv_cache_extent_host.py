@@ -52,3 +52,11 @@ def test_every_order_is_taken_and_none_that_overlaps(order):
     for d in order:                                # a stride eight less: one thing begins inside another one
         assert status(**dict(strides, **{DIMS[d][1]: strides[DIMS[d][1]] - 8})) == SHAPE
         assert status(**dict(strides, **{DIMS[d][0]: 1, DIMS[d][1]: 0})) == OK       # of which there is one: any stride
+
+
+@pytest.mark.parametrize("n_pages", [(1 << 31) - 1023, (1 << 31) - 512, (1 << 31) - 1])
+def test_more_pages_than_the_lists_can_number(n_pages):
+    """Lists are made in chunks of 1024 pages, numbered in 32 bits: the last chunk has to end below 2^31."""
+    assert status(n_pages=n_pages, n_layers=1) == LARGE
+    assert L.lora_kv_moves_ws_bytes(n_pages, 4) == 0
+    assert L.lora_kv_moves_ws_bytes((1 << 31) - 1024, 4) > 16 << 31
