@@ -611,6 +611,12 @@ def _int32(t, what, shape):
     return t
 
 
+def _holds_int32(t, what, n):
+    """A tensor that a call reads or writes n int32 of; what is no tensor is an address and goes as it is."""
+    if hasattr(t, "is_contiguous") and (t.element_size() != 4 or t.is_floating_point() or not t.is_contiguous() or t.numel() < n):
+        raise ValueError(f"{what}: a contiguous int32 tensor of {n} elements at least, got {t.dtype} {list(t.shape)}")
+
+
 class KvBatch:
     """lora_kv_batch over int32 device tensors: row_start [n_seqs + 1], seq_len [n_seqs], table
     [n_seqs][max_pages], position [n_rows] or None.  Holds the tensors and a status word."""
@@ -698,6 +704,9 @@ class KvMoves:
 
 def lora_kv_plan(cache: KvCache, state: KvState, to: KvState, src, new_len, moves: KvMoves, stream=None):
     """src, new_len: int32 device tensors [n_seqs]."""
+    n = 0 if to is None else to.c.n_seqs
+    _holds_int32(src, "src", n)
+    _holds_int32(new_len, "new_len", n)
     rc = _calls().kv_plan(cache, state, to, src, new_len, moves, stream)
     if rc:
         _check(rc, "lora_kv_plan")

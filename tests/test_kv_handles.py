@@ -1,0 +1,26 @@
+"""What the binding of the paged cache refuses before a call: tensors of another type or size than the device code reads and writes."""
+import pytest
+import torch
+
+import paper_2604_07173_amd as L
+
+
+def i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def setup(n_pages=10, n_seqs=3):
+    k = torch.zeros((1, n_pages, 2, 16, 8), dtype=torch.bfloat16)
+    states = [L.KvState(i32(n_seqs, 4), i32(n_seqs), i32(n_pages)) for _ in range(2)]
+    return L.KvCache(k, k.clone()), states[0], states[1], L.KvMoves(n_pages, n_seqs, device="cpu")
+
+
+@pytest.mark.parametrize("bad", [
+    torch.zeros(3, dtype=torch.int64), torch.zeros(3), torch.zeros(3, dtype=torch.int16), i32(2), i32(0), i32(6)[::2]])
+@pytest.mark.parametrize("which", [0, 1])
+def test_a_plan_of_other_types_and_sizes(bad, which):
+    cache, state, to, moves = setup()
+    args = [i32(3), i32(3)]
+    args[which] = bad
+    with pytest.raises(ValueError, match=("src", "new_len")[which]):
+        L.lora_kv_plan(cache, state, to, *args, moves, stream=0)
