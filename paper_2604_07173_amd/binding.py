@@ -685,6 +685,7 @@ class KvState:
         n = seq_len.shape[0]
         self.table, self.seq_len = _int32(table, "table", (n, table.shape[-1])), _int32(seq_len, "seq_len", (n,))
         self.page_ref = None if page_ref is None else _int32(page_ref, "page_ref", (page_ref.shape[0],))
+        self.counted = LORA_KV_MAX_PAGES if page_ref is None else page_ref.shape[0]      # pages that it has room for
         self.c = _KvState(n, table.shape[1], table.data_ptr(), seq_len.data_ptr(), _addr(page_ref))
 
 
@@ -702,17 +703,25 @@ class KvMoves:
                           self.ws.data_ptr(), self.ws.numel())
 
 
+def _count_all_pages(cache, *states):
+    for s in states:
+        if isinstance(s, KvState) and cache is not None and s.counted < cache.c.n_pages:
+            raise ValueError(f"page_ref: one int32 for each of the cache's {cache.c.n_pages} pages, got {s.counted}")
+
+
 def lora_kv_plan(cache: KvCache, state: KvState, to: KvState, src, new_len, moves: KvMoves, stream=None):
     """src, new_len: int32 device tensors [n_seqs]."""
     n = 0 if to is None else to.c.n_seqs
     _holds_int32(src, "src", n)
     _holds_int32(new_len, "new_len", n)
+    _count_all_pages(cache, state, to)
     rc = _calls().kv_plan(cache, state, to, src, new_len, moves, stream)
     if rc:
         _check(rc, "lora_kv_plan")
 
 
 def lora_kv_compact(cache: KvCache, state: KvState, to: KvState, moves: KvMoves, stream=None):
+    _count_all_pages(cache, state, to)
     rc = _calls().kv_compact(cache, state, to, moves, stream)
     if rc:
         _check(rc, "lora_kv_compact")

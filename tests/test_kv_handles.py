@@ -24,3 +24,17 @@ def test_a_plan_of_other_types_and_sizes(bad, which):
     args[which] = bad
     with pytest.raises(ValueError, match=("src", "new_len")[which]):
         L.lora_kv_plan(cache, state, to, *args, moves, stream=0)
+
+
+@pytest.mark.parametrize("short", [0, 1])
+@pytest.mark.parametrize("compact", [False, True])
+def test_fewer_counts_than_the_cache_has_pages(short, compact):
+    """page_ref is written (in `from`: read, where a plan is refused) for every page of the cache."""
+    cache, state, to, moves = setup()
+    states = [state, to]
+    states[short] = L.KvState(i32(3, 4), i32(3), i32(9))
+    with pytest.raises(ValueError, match="page_ref"):
+        if compact:
+            L.lora_kv_compact(cache, *states, moves, stream=0)
+        else:
+            L.lora_kv_plan(cache, *states, i32(3), i32(3), moves, stream=0)
