@@ -592,12 +592,13 @@ def lora_moe_down_combine(pool, layer, hmid, ld_in, adapter_id, expert_id, seg: 
 
 class KvCache:
     """lora_kv_cache over two tensors seen as [layer][page][head][token][width], in any order in memory
-    (bf16, the same strides, the width contiguous).  Holds the tensors."""
+    (bf16 or its bits as 16-bit integers, the same strides, the width contiguous).  Holds the tensors."""
 
     def __init__(self, k, v):
-        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.stride(4) != 1 or k.element_size() != 2 \
-                or v.element_size() != 2:
-            raise ValueError("k and v: [layer][page][head][token][width] of 16 bits, alike in shape and strides")
+        import torch
+        bf16 = all(t.dtype in (torch.bfloat16, torch.int16, torch.uint16) for t in (k, v))
+        if not bf16 or k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.stride(4) != 1:
+            raise ValueError("k and v: bf16 [layer][page][head][token][width], alike in shape and strides")
         self.k, self.v = k, v
         c = self.c = _KvCache()
         c.k, c.v = k.data_ptr(), v.data_ptr()

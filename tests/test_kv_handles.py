@@ -38,3 +38,12 @@ def test_fewer_counts_than_the_cache_has_pages(short, compact):
             L.lora_kv_compact(cache, *states, moves, stream=0)
         else:
             L.lora_kv_plan(cache, *states, i32(3), i32(3), moves, stream=0)
+
+
+def test_a_cache_of_another_16_bit_type():
+    k = torch.zeros((1, 4, 2, 16, 8), dtype=torch.float16)
+    for pair in ((k, k.clone()), (k.bfloat16(), k), (k, k.bfloat16())):
+        with pytest.raises(ValueError, match="bf16"):
+            L.KvCache(*pair)
+    for kind in (torch.bfloat16, torch.int16):                 # the type, or its bits
+        assert L.KvCache(k.to(kind), k.to(kind)).c.head_dim == 8
