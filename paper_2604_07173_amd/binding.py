@@ -629,6 +629,7 @@ class KvBatch:
         self.table = _int32(table, "table", (n, table.shape[-1]))
         self.position = None if position is None else _int32(position, "position", (n_rows,))
         self.status = torch.zeros(1, dtype=torch.int32, device=seq_len.device) if status is None else status
+        _holds_int32(self.status, "status", 1)
         c = self.c = _KvBatch()
         c.n_seqs, c.n_rows, c.max_rows, c.max_pages = n, int(n_rows), int(max_rows), table.shape[1]
         c.row_start, c.seq_len, c.table = row_start.data_ptr(), seq_len.data_ptr(), table.data_ptr()

@@ -47,3 +47,15 @@ def test_a_cache_of_another_16_bit_type():
             L.KvCache(*pair)
     for kind in (torch.bfloat16, torch.int16):                 # the type, or its bits
         assert L.KvCache(k.to(kind), k.to(kind)).c.head_dim == 8
+
+
+@pytest.mark.parametrize("bad", [torch.zeros(1), i32(0), torch.zeros(1, dtype=torch.int16), torch.zeros(4, dtype=torch.uint8)])
+def test_a_status_of_another_type(bad):
+    """The calls set bits of a 32-bit word there."""
+    with pytest.raises(ValueError, match="status"):
+        L.KvBatch(i32(4), i32(3), i32(3, 2), 3, status=bad)
+
+
+@pytest.mark.parametrize("good", [i32(1), i32(), i32(5)[2:3], torch.zeros(1, dtype=torch.uint32)])
+def test_a_status_word(good):
+    assert L.KvBatch(i32(4), i32(3), i32(3, 2), 3, status=good).c.status == good.data_ptr()
