@@ -11,33 +11,20 @@
 // Long tiles are work items of their own; where there are few, their tokens are cut evenly into several items.
 #pragma once
 #include "kv_device.h"
+#include "kv_work.h"
 
 namespace lora {
 
-constexpr int kLongTile = 128;           // rows
-constexpr int kUnitShift = 7;            // a unit is 128 tokens: a step of a workgroup's four waves
-constexpr float kMostUnits = 1 << 29;    // on the line; units are doubled until there are no more
-constexpr int kMostBlocks = 768;         // workgroups of short tiles: three on every CU
-// Items of long tiles that fill the chip: one on every CU.  Two fit, but the second adds less than writing and joining the parts
-// of more cuts costs (4 chunks of 64 rows over 2000 tokens, 32 / 8 heads: 34.5 us, with twice the items 37.4; 2 chunks of 512 rows
-// over 1500: 56 and 74; 8 of 128 over 500: 27 and 50; one of 200 over 8000: 58.7 and 55.8)
-constexpr int kLongTarget = 256;
-constexpr int kLongMinSplit = 512;       // tokens of a cut range at least
-// rows x group up to which a sequence goes in short tiles, where all have as many and where they differ.  Long tiles are faster
-// from 33 on (32 sequences of 12 rows and 4 heads each over 1500 tokens 64.7 / 49.3 us in short / long tiles), but a batch of both
-// takes two kernels, one after the other (48 uneven sequences of up to 13 rows, 5 x 4 heads of 80: 38.2 us in short tiles, 49.8
-// in both)
-constexpr int kShortEqual = 32, kShortLimit = 64;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kInlineSeqs = 256;         // sequences up to which every workgroup makes the plan for itself, in LDS: one launch less
 
 enum Kind { kShort, kLong };
 
 // The plan: a head of kPlanHead words, then kPlanArrays arrays over the sequences: units of short tiles before each
 // sequence, work items and partial results of long tiles, and rows x heads of long tiles to join; then the sequences
 // themselves.
-enum { kUnits, kShare, kUnitTokens, kChunk, kItems, kJoinUnits, kPlanHead = 8 };
-enum { kBaseUnit, kBaseItem, kBaseSlot, kBaseJoin, kPlanSums, kSeqRow0 = kPlanSums, kSeqRows, kSeqLen, kPlanArrays };
+enum { kUnits, kShare, kUnitTokens, kChunk, kItems, kJoinUnits, kHeadWords };
+enum { kBaseUnit, kBaseItem, kBaseSlot, kBaseJoin, kPlanSums, kSeqRow0 = kPlanSums, kSeqRows, kSeqLen, kSeqArrays };
+static_assert(kHeadWords <= kPlanHead && kSeqArrays == kPlanArrays, "as many words as the host makes room for");
 constexpr int kInlineWords = kPlanHead + kPlanArrays * kInlineSeqs;
 
 struct Seq {

@@ -455,51 +455,6 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
     }
 }
 
-size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
-
-// Which kernels a batch takes, and upper bounds of their work, from what the host knows.
-struct Kinds {
-    bool has_short, has_long;
-    int limit;                            // rows x group of a sequence that goes in short tiles
-    int shift;                            // rows of a short tile, as a power of two
-    int blocks;                           // workgroups that share the short tiles
-    int64_t long_items;
-};
-
-Kinds kinds_of(int n_seqs, int n_rows, int max_rows, int heads, int kv_heads, int dim)
-{
-    const int64_t group = heads / kv_heads;
-    const int64_t most = max_rows > 0 ? std::min(max_rows, n_rows) : n_rows;
-    Kinds k;
-    const bool equal = max_rows > 0 && (int64_t)max_rows * n_seqs == n_rows;
-    k.has_long = most * group > (equal ? kShortEqual : kShortLimit);
-    k.has_short = !k.has_long || !equal;
-    // a sequence with more rows than the host thought still has to go somewhere
-    k.limit = !k.has_long ? INT_MAX : !k.has_short ? 0 : kShortLimit;
-    k.shift = !k.has_long && most * group > 16 && dim <= 128 ? 5 : 4;
-    k.blocks = dim <= 128 && k.shift == 4 ? kMostBlocks : kMostBlocks / 3 * 2;
-    const int64_t some = std::min(n_seqs, n_rows);
-    k.long_items = kLongTarget + kv_heads * (some + n_rows * group / kLongTile);
-    return k;
-}
-
-struct Ws {
-    size_t plan, short_ml, short_o, long_ml, long_o, bytes;
-};
-
-Ws ws_of(int n_seqs, const Kinds &k, int dim)
-{
-    const size_t rows_s = k.has_short ? 2 * (size_t)k.blocks << k.shift : 0, rows_l = k.has_long ? 2 * (size_t)kLongTarget * kLongTile : 0;
-    Ws w;
-    w.plan = 0;
-    w.short_ml = up256((kPlanHead + kPlanArrays * (size_t)n_seqs) * 4);
-    w.short_o = w.short_ml + up256(rows_s * 8);
-    w.long_ml = w.short_o + up256(rows_s * dim * 4);
-    w.long_o = w.long_ml + up256(rows_l * 8);
-    w.bytes = w.long_o + up256(rows_l * dim * 4);
-    return w;
-}
-
 template <int DP, int MT, int BLOCKS>
 void launch_attend(const AttnParams &p, unsigned grid, hipStream_t s)
 {
@@ -511,13 +466,13 @@ void launch_attend(const AttnParams &p, unsigned grid, hipStream_t s)
 
 size_t attention_ws_bytes(int n_seqs, int n_rows, int max_rows, int heads, int kv_heads, int dim)
 {
-    return ws_of(n_seqs, kinds_of(n_seqs, n_rows, max_rows, heads, kv_heads, dim), dim).bytes;
+    return attn_ws_of(n_seqs, kinds_of(n_seqs, n_rows, max_rows, heads, kv_heads, dim), dim).bytes;
 }
 
 hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s)
 {
     const Kinds k = kinds_of(p.b.n_seqs, p.b.n_rows, max_rows, p.heads, p.c.n_heads, p.c.dim);
-    const Ws at = ws_of(p.b.n_seqs, k, p.c.dim);
+    const AttnWs at = attn_ws_of(p.b.n_seqs, k, p.c.dim);
     char *w = static_cast<char *>(ws);
     p.plan = reinterpret_cast<int32_t *>(w + at.plan);
     p.part_ml = reinterpret_cast<float *>(w + at.short_ml);
@@ -529,7 +484,7 @@ hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s
     p.short_blocks = k.blocks;
     if (p.b.n_seqs > kInlineSeqs) hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
     if (k.has_long) {
-        const hipError_t e = launch_attend_long(p, (int)std::min<int64_t>(k.long_items, INT_MAX), s);
+        const hipError_t e = launch_attend_long(p, (int)k.long_items, s);
         if (e != hipSuccess) return e;
     }
     const int64_t reach = p.window ? std::min<int64_t>(p.b.tokens_max, (int64_t)p.window + kLongTile) : p.b.tokens_max;
