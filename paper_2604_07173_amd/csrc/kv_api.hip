@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "kv_internal.h"
 #include "kv_layout.h"
@@ -274,7 +275,8 @@ int lora_kv_attention(const lora_kv_cache *cache, int layer, const lora_kv_batch
     p.lse = lse;
     p.ldq = ldq;
     p.ldo = ldo;
-    p.scale_log2 = (float)(scale * 1.4426950408889634);
+    // below infinity: equal scores stay equal, and all others are further apart than any weight shows
+    p.scale_log2 = (float)std::min(scale * 1.4426950408889634, (double)std::numeric_limits<float>::max());
     p.heads = n_heads;
     p.group = n_heads / cache->n_heads;
     p.group_div = fast_div(p.group);
