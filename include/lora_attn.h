@@ -142,12 +142,13 @@ int lora_rope_append(const lora_kv_cache *cache, int layer, const lora_kv_batch 
  * (causal only) only j > p - window.  A row that sees nothing gives zeros.  q, out: bf16, row
  * strides ldq, ldo in elements, multiples of 8, not overlapping.  lse: device fp32
  * [n_rows][n_heads] or NULL, the natural logarithm of the sum of exp(scale * q . K), -inf for a
- * row that sees nothing.  scale: finite, > 0.  What pages hold past a sequence's length, and tokens
- * that a row does not see, have no effect on it, NaN and infinities included.  Scores, softmax
- * sums and output sums are fp32, the softmax weights are rounded to bf16 for the product with V.
- * Results are bit-identical run to run.  A length below zero or beyond the table raises
- * LORA_STATUS_BAD_LENGTH and is taken for the nearest that is not, a table entry that is no page
- * LORA_STATUS_BAD_PAGE; that sequence's rows mean nothing then.
+ * row that sees nothing.  n_rows * n_heads: at most 2^29 (LORA_ERR_TOO_LARGE).  scale: finite, > 0.
+ * What pages hold past a sequence's length, and tokens that a row does not see, have no effect on it,
+ * NaN and infinities included; an infinity or NaN of V that it does see makes that element of its
+ * output infinite or NaN.  Scores, softmax sums and output sums are fp32, the softmax weights are
+ * rounded to bf16 for the product with V.  Results are bit-identical run to run.  A length below zero
+ * or beyond the table raises LORA_STATUS_BAD_LENGTH and is taken for the nearest that is not, a table
+ * entry that is no page LORA_STATUS_BAD_PAGE; that sequence's rows mean nothing then.
  * ws: device scratch of lora_kv_attention_ws_bytes, which depends on the cache's heads, the
  * batch's n_seqs, n_rows and max_rows, and n_heads, not on lengths.
  * ------------------------------------------------------------------------------------ */

@@ -8,7 +8,8 @@
 // the sum and the rescaling need no exchange but one across the four lane groups, and the lanes that hold
 // P as the result of the first product hold it as the operand of the second: the 32 tokens go into
 // the second product in the order in which the first left them (group g: tokens 4g .. 4g+3 and
-// 16+4g .. 16+4g+3).  V is read transposed from LDS in that order (ds_read_b64_tr_b16), where it has come straight from
+// 16+4g .. 16+4g+3).  The weights, at most 1, are rounded to bf16 there, the type that the products take: an error of 2^-8 of each at
+// most, as much as K and V themselves come with; their sum takes them unrounded.  V is read transposed from LDS in that order (ds_read_b64_tr_b16), where it has come straight from
 // memory; K goes from memory into the operand registers.
 //
 // Bound by the reading of K and V from about 100 MB on: 32 / 8 heads of 128, 256 users with 100 to 4000 tokens (1.17 GB) 208 us in
@@ -283,7 +284,8 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
                     for (int mt = 0; mt < MT; ++mt)
                         o[mt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[mt], o[mt][d] * shrink[mt], 0, 0, 0);
                 }
-                // the rest reaches the rows that see it: whatever the weight, infinity or NaN stays what it is
+                // the rest is added as it is to the rows that see it.  In blocks without hidden tokens the product does so, but for
+                // a weight that has become zero, with which infinity is NaN; so is a sum of infinity that is scaled by zero later
 #pragma unroll 1
                 for (int j = 0; j < kBlock; ++j)
 #pragma unroll

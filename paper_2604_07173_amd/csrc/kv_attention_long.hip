@@ -3,7 +3,8 @@
 // K and V of 64 tokens at a time go straight into LDS, where all waves read them, while the 64 before are
 // worked on.  S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16, as in kv_attention.hip: a lane's column is one row
 // of the tile, its two lane halves hold different tokens, and P goes from the first product's result to the second
-// one's operand without leaving its lane (16 tokens: 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 for lane half h).
+// one's operand without leaving its lane (16 tokens: 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 for lane half h).  The weights are
+// rounded to bf16 for it as there: 2^-8 of each at most; their sum takes them unrounded.
 //
 // Weights need not be taken against the running maximum, only against a value near it: the reference is the maximum of the
 // first tokens that a row sees, and moves to the running one when the weights of a step pass 2^10.  So most steps look for
@@ -280,7 +281,8 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_part(v_tile(k, d)), pf[k], o[d], 0, 0, 0);
-            // the rest reaches the rows that see it: whatever the weight, infinity or NaN stays what it is
+            // the rest is added as it is to the rows that see it.  In steps without hidden tokens the product does so, but for a
+            // weight that has become zero, with which infinity is NaN; so is a sum of infinity that is scaled by zero later
 #pragma unroll 1
             for (int j = 0; j < kTokens; ++j) {
                 if (j0 + j < see_lo || j0 + j >= see_hi) continue;

@@ -20,9 +20,11 @@ constexpr int kLongTarget = 256;
 constexpr int kMostItems = (1 << 24) - 1;    // workgroups of 256 threads: a launch has less than 2^32 threads
 constexpr int kLongMinSplit = 512;       // tokens of a cut range at least
 // rows x group up to which a sequence goes in short tiles, where all have as many and where they differ.  Long tiles are faster
-// from 33 on (32 sequences of 12 rows and 4 heads each over 1500 tokens 64.7 / 49.3 us in short / long tiles), but a batch of both
-// takes two kernels, one after the other (48 uneven sequences of up to 13 rows, 5 x 4 heads of 80: 38.2 us in short tiles, 49.8
-// in both)
+// from 33 on where there are many sequences (32 of 12 rows and 4 heads each over 1500 tokens: 64.7 / 49.3 us in short / long tiles; 128 of 9
+// to 16 rows over 300 - 4000: 286 - 324 / 179 - 196), and so for one new row of 34 to 64 heads that share K and V (64 sequences
+// over 100 - 8000 tokens 36 - 41 / 25 - 29 us, 256 of them 94 - 108 / 74 - 87, three over 80000 55 / 41; but 8 of them 14 - 21 / 22 - 23, one 9 - 13 /
+// 10 - 21).  A batch of both takes two kernels, one after the other (48 uneven sequences of up to 13 rows, 5 x 4 heads of
+// 80: 38.2 us in short tiles, 49.8 in both).
 constexpr int kShortEqual = 32, kShortLimit = 64;
 constexpr int kInlineSeqs = 256;         // sequences up to which every workgroup makes the plan for itself, in LDS: one launch less
 // 32-bit words of the plan in memory: of its head, and of each sequence
@@ -57,6 +59,8 @@ inline Kinds kinds_of(int n_seqs, int n_rows, int max_rows, int heads, int kv_he
         k.long_items = kLongTarget + kv_heads * (seqs + n_rows * group / kLongTile);
         if (!equal || !k.has_long || k.long_items <= kMostItems) break;
     }
+    // Beside long chunks the others are taken for decoding users, in tiles of 16 rows: 64 of them with one or two rows of 4 heads 274
+    // and 287 us for the batch, in tiles of 32 297 and 307; with 5 rows 340 and 314, 12 rows 436 and 415, 16 rows 468 and 385; 8 of any 0 to 3 us apart.
     k.shift = !k.has_long && most * group > 16 && dim <= 128 ? 5 : 4;
     k.blocks = dim <= 128 && k.shift == 4 ? kMostBlocks : kMostBlocks / 3 * 2;
     return k;
