@@ -6,8 +6,8 @@
 //
 // Every element is read once and written once, so the kernel is bound by memory (by the latency of finding a
 // row's sequence and page for small batches).  A workgroup takes one row: its waves find the place of the row
-// and the cosines, which all heads share, and pass them on through LDS.  16384 rows of 32 + 8 + 8 heads of 128 take 76 us,
-// 5.3 TB/s, more than a plain copy of as much (4.85); 64 rows 4.1 us.
+// and the cosines, which all heads share, and pass them on through LDS.  16384 rows of 32 + 8 + 8 heads of 128 take 77 us,
+// 5.2 TB/s, more than a plain copy of as much (4.85); 64 rows 4.1 us.
 #include "kv_device.h"
 
 namespace lora {

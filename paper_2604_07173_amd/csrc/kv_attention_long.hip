@@ -10,10 +10,11 @@
 // first tokens that a row sees, and moves to the running one when the weights of a step pass 2^10.  So most steps look for
 // no maximum and rescale nothing; the sums are the same up to rounding.
 //
-// Measured, 32 / 8 heads of 128: 8 prompts of 2048 rows 365 us, 750 TFLOP/s of the visible pairs; 1984 rows over 18000 tokens 626 us,
-// 870 TFLOP/s, where the clock falls to 1.93 GHz (a large library product reaches 1369 TFLOP/s on this card).  Of the SIMDs' time
-// there the products take 43 % and vector instructions 52 %, LDS is busy for 64 % (K 8 cycles a read
-// of 1 KiB, V 8 cycles a transposed read of 512 bytes).
+// Measured, 32 / 8 heads of 128: 8 prompts of 2048 rows 357 us, 770 TFLOP/s of the visible pairs; 1984 rows over 18000 tokens 585 us,
+// 930 TFLOP/s (a large library product reaches 1369 TFLOP/s on this card).  That is once the clock has settled under such work: the first twenty
+// launches after idling take 394 - 490 and 615 - 719 us.  Of the SIMDs' time in the second the products take 44 % and vector instructions
+// 53 %: of about 250 per step 117 form the weights, 64 copy the outputs' registers around the product with V, 48 form addresses
+// of loads.  LDS is busy for 66 % (K 8 cycles a read of 1 KiB, V 8 cycles a transposed read of 512 bytes).
 // Tried and left out, as slower: 64 rows per wave, which halves the LDS reads but needs 512 registers, between whose two
 // halves the compiler moves the outputs at every branch (2.2 ms; 377 us with 32); a step's scores formed while the weights of
 // the step before are (spills, 564 us), or its products of both kinds in one stretch (453 us); eight waves on K and V (a batch
