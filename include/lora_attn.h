@@ -159,6 +159,56 @@ int lora_kv_attention(const lora_kv_cache *cache, int layer, const lora_kv_batch
                       float scale, int causal, int window, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------
+ * Sequences that hold the same first pages (several answers to one prompt, lora_kv_plan's forks), and attention that
+ * reads such pages once for all of them.
+ *
+ * lora_kv_share finds them in a batch's tables.  Sequence s takes part if it has 1 .. max_rows new rows (max_rows 0: any
+ * number) and at least min_pages (>= 1) whole pages before the first of them.  Its leader is the lowest sequence that takes
+ * part and has the same table entry min_pages - 1; it joins the leader's group if their first min_pages entries are all the same.  Two or
+ * more make a group, whose shared tokens are the whole pages that every member has before its new rows and that agree, place by place,
+ * with the leader's.  Groups are numbered by their leaders, members and rows stay in order:
+ *   groups[g] = { leader, shared tokens, first entry in rows, number of rows }, { -1, 0, 0, 0 } behind the last
+ *   rows      the new rows of the groups, one group after another, -1 behind the last
+ *   own[s]    shared tokens of s's group, 0 if in none;  place[s]: the entry of s's first new row in rows, or -1
+ *   counts    groups, their rows, their members, and tokens that need not be read again (at most 2^31 - 1)
+ * A length that makes no sense raises LORA_STATUS_BAD_LENGTH in the batch's status word and its sequence takes no part; rows that are no
+ * partition raise it too, and there is no group then.  One launch for small batches, else three.  The result holds for all layers
+ * of a step.  It may also be written by other means, as long as it says the truth.
+ *
+ * lora_kv_attention_shared is lora_kv_attention without a window for a batch with its groups: a group's shared tokens are
+ * taken from its leader's table, and the entries for them in the others' tables are not looked at.  Bits may differ from
+ * lora_kv_attention's, as sums are taken in another order; they are the same from run to run.  What `shared` says wrongly makes the results of the
+ * rows concerned mean nothing, and nothing is read or written out of bounds.  n_rows * n_heads and the same of shared->n_rows: at most 2^26
+ * (LORA_ERR_TOO_LARGE).  ws depends on what lora_kv_attention_ws_bytes depends on, and on shared's n_rows and max_group_rows.
+ * ------------------------------------------------------------------------------------ */
+typedef struct lora_kv_shared {
+    int32_t n_seqs;           /* sequences of the batch */
+    int32_t n_rows;           /* entries of rows: at least the batch's n_rows, or n_seqs * max_rows if that is less */
+    int32_t max_group_rows;   /* rows of the largest group as far as the host knows, 0 = unknown; decides which
+                                 kernels run, as max_rows of a batch does */
+    int32_t reserved;
+    int32_t *groups;          /* device [n_seqs / 2, at least 1][4] */
+    int32_t *rows;            /* device [n_rows] */
+    int32_t *own, *place;     /* device [n_seqs] */
+    int32_t *counts;          /* device [4] */
+    void *ws;                 /* device scratch of lora_kv_share_ws_bytes; lora_kv_share only */
+    size_t ws_bytes;
+} lora_kv_shared;
+
+size_t lora_kv_share_ws_bytes(int n_seqs);
+
+int lora_kv_share(const lora_kv_cache *cache, const lora_kv_batch *batch, const lora_kv_shared *shared,
+                  int min_pages, int max_rows, void *stream);
+
+size_t lora_kv_attention_shared_ws_bytes(const lora_kv_cache *cache, const lora_kv_batch *batch,
+                                         const lora_kv_shared *shared, int n_heads);
+
+int lora_kv_attention_shared(const lora_kv_cache *cache, int layer, const lora_kv_batch *batch,
+                             const lora_kv_shared *shared, const void *q, int64_t ldq, int n_heads, void *out,
+                             int64_t ldo, float *lse, float scale, int causal, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/* ------------------------------------------------------------------------------------
  * Pages.  A state says which pages the sequences in its n_seqs slots hold: the first
  * ceil(seq_len / page_size) entries of a slot's table row.  Slots may share pages (a common
  * prompt); page_ref counts the slots that hold a page, 0 = free.  Prefixes that outlive their

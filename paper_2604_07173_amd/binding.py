@@ -32,6 +32,7 @@ EXPORTED_SYMBOLS = [
     "lora_expand", "lora_apply", "lora_group_ws_bytes", "lora_group_launches", "lora_apply_group", "lora_build_apply_group", "lora_build_apply_launches", "lora_moe_ws_bytes", "lora_moe_apply", "lora_moe_build_apply", "lora_moe_apply_static", "lora_moe_combine_ws_bytes", "lora_moe_down_combine", "lora_moe_shrink", "lora_moe_expand",
     "lora_rope_freqs", "lora_rope_append", "lora_kv_attention_ws_bytes", "lora_kv_attention", "lora_kv_moves_ws_bytes",
     "lora_kv_plan", "lora_kv_compact", "lora_kv_copy_pages",
+    "lora_kv_share_ws_bytes", "lora_kv_share", "lora_kv_attention_shared_ws_bytes", "lora_kv_attention_shared",
 ]
 
 
@@ -83,6 +84,12 @@ class _RopeDesc(C.Structure):
 class _Rope(C.Structure):
     _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int32), ("pairing", C.c_int32), ("amplitude", C.c_float),
                 ("reserved", C.c_int32)]
+
+
+class _KvShared(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_group_rows", C.c_int32), ("reserved", C.c_int32),
+                ("groups", C.c_void_p), ("rows", C.c_void_p), ("own", C.c_void_p), ("place", C.c_void_p), ("counts", C.c_void_p),
+                ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
 
 
 class _KvState(C.Structure):
@@ -215,6 +222,15 @@ def load_library():
     lib.lora_kv_attention.restype = i32
     lib.lora_kv_attention.argtypes = [C.POINTER(_KvCache), i32, C.POINTER(_KvBatch), vp, i64, i32, vp, i64, vp, C.c_float,
                                       i32, i32, vp, sz, vp]
+    lib.lora_kv_share_ws_bytes.restype = sz
+    lib.lora_kv_share_ws_bytes.argtypes = [i32]
+    lib.lora_kv_share.restype = i32
+    lib.lora_kv_share.argtypes = [C.POINTER(_KvCache), C.POINTER(_KvBatch), C.POINTER(_KvShared), i32, i32, vp]
+    lib.lora_kv_attention_shared_ws_bytes.restype = sz
+    lib.lora_kv_attention_shared_ws_bytes.argtypes = [C.POINTER(_KvCache), C.POINTER(_KvBatch), C.POINTER(_KvShared), i32]
+    lib.lora_kv_attention_shared.restype = i32
+    lib.lora_kv_attention_shared.argtypes = [C.POINTER(_KvCache), i32, C.POINTER(_KvBatch), C.POINTER(_KvShared), vp, i64, i32, vp,
+                                             i64, vp, C.c_float, i32, vp, sz, vp]
     lib.lora_kv_moves_ws_bytes.restype = sz
     lib.lora_kv_moves_ws_bytes.argtypes = [i32, i32]
     lib.lora_kv_plan.restype = i32
@@ -231,6 +247,7 @@ def load_library():
     addresses = {name: C.cast(getattr(lib, name), vp).value for name in EXPORTED_SYMBOLS}
     calls.bind(addresses, _stream)
     calls.bind_kv(addresses)
+    calls.bind_shared(addresses)
     _pycall = calls
     _lib = lib
     return lib
@@ -674,6 +691,40 @@ def lora_kv_attention(cache: KvCache, layer: int, batch: KvBatch, q, ldq, n_head
     rc = _calls().kv_attention(cache, layer, batch, q, ldq, n_heads, out, ldo, lse, scale, causal, window, ws, stream)
     if rc:
         _check(rc, "lora_kv_attention")
+
+
+def lora_kv_share_ws_bytes(n_seqs: int) -> int:
+    return int(load_library().lora_kv_share_ws_bytes(n_seqs))
+
+
+class KvShared:
+    """Device buffers of a lora_kv_shared for batches of n_seqs sequences whose groups have up to n_rows new rows together."""
+
+    def __init__(self, n_seqs: int, n_rows: int, max_group_rows: int = 0, device="cuda"):
+        import torch
+        i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)                        # noqa: E731
+        self.groups, self.rows = i32(max(n_seqs // 2, 1), 4), i32(n_rows)
+        self.own, self.place, self.counts = i32(n_seqs), i32(n_seqs), i32(4)
+        self.ws = torch.empty(max(lora_kv_share_ws_bytes(n_seqs), 256), dtype=torch.uint8, device=device)
+        self.c = _KvShared(n_seqs, n_rows, max_group_rows, 0, self.groups.data_ptr(), self.rows.data_ptr(), self.own.data_ptr(),
+                           self.place.data_ptr(), self.counts.data_ptr(), self.ws.data_ptr(), self.ws.numel())
+
+
+def lora_kv_share(cache: KvCache, batch: KvBatch, shared: KvShared, min_pages: int = 1, max_rows: int = 0, stream=None):
+    rc = _calls().kv_share(cache, batch, shared, min_pages, max_rows, stream)
+    if rc:
+        _check(rc, "lora_kv_share")
+
+
+def lora_kv_attention_shared_ws_bytes(cache: KvCache, batch: KvBatch, shared: KvShared, n_heads: int) -> int:
+    return int(load_library().lora_kv_attention_shared_ws_bytes(_c(cache), _c(batch), _c(shared), n_heads))
+
+
+def lora_kv_attention_shared(cache: KvCache, layer: int, batch: KvBatch, shared: KvShared, q, ldq, n_heads: int, out, ldo, lse,
+                             scale: float, ws, causal: bool = True, stream=None):
+    rc = _calls().kv_attention_shared(cache, layer, batch, shared, q, ldq, n_heads, out, ldo, lse, scale, causal, ws, stream)
+    if rc:
+        _check(rc, "lora_kv_attention_shared")
 
 
 def lora_kv_moves_ws_bytes(n_pages: int, n_seqs: int) -> int:

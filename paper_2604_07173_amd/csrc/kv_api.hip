@@ -9,6 +9,7 @@
 
 #include "kv_internal.h"
 #include "kv_layout.h"
+#include "kv_work.h"
 
 using namespace lora;
 
@@ -113,6 +114,50 @@ KvRows rows_of(const lora_kv_batch *b, int page_size)
     const int64_t room = (int64_t)b->max_pages * page_size;
     r.tokens_max = (int)(room < (1 << 30) ? room : (1 << 30));     // offsets inside a sequence stay far below 2^31
     return r;
+}
+
+// What both calls of a batch with groups look at.
+int check_shared(const lora_kv_shared *s, const lora_kv_batch *b)
+{
+    if (!s || s->n_seqs < 0 || s->n_rows < 0 || s->max_group_rows < 0) return LORA_ERR_INVALID_ARG;
+    if (s->n_seqs > LORA_MAX_ROWS_LONG || s->n_rows > LORA_MAX_ROWS_LONG) return LORA_ERR_TOO_LARGE;
+    if (b->n_rows == 0) return LORA_OK;
+    if (!s->groups || !s->own || !s->place || !s->counts || (s->n_rows > 0 && !s->rows)) return LORA_ERR_INVALID_ARG;
+    if (s->n_seqs != b->n_seqs) return LORA_ERR_BAD_SHAPE;
+    return LORA_OK;
+}
+
+int check_attention(const void *q, int64_t ldq, const void *out, int64_t ldo, const float *lse, int64_t width, const void *ws)
+{
+    int rc;
+    if ((rc = check_rows(q, ldq, width)) != LORA_OK) return rc;
+    if ((rc = check_rows(out, ldo, width)) != LORA_OK) return rc;
+    if (q == out || !ws) return LORA_ERR_INVALID_ARG;
+    if (!aligned(ws, 16) || !aligned(lse, 4)) return LORA_ERR_MISALIGNED;
+    return LORA_OK;
+}
+
+AttnParams attention_params(const lora_kv_cache *cache, int layer, const lora_kv_batch *batch, const void *q, int64_t ldq, int n_heads,
+                            void *out, int64_t ldo, float *lse, float scale, int causal)
+{
+    AttnParams p;
+    memset(&p, 0, sizeof p);
+    p.c = view_of(cache, layer);
+    p.b = rows_of(batch, cache->page_size);
+    p.q = static_cast<const uint16_t *>(q);
+    p.out = static_cast<uint16_t *>(out);
+    p.lse = lse;
+    p.ldq = ldq;
+    p.ldo = ldo;
+    // below infinity: equal scores stay equal, and all others are further apart than any weight shows
+    p.scale_log2 = (float)std::min(scale * 1.4426950408889634, (double)std::numeric_limits<float>::max());
+    p.heads = n_heads;
+    p.group = n_heads / cache->n_heads;
+    p.group_div = fast_div(p.group);
+    p.kv_div = fast_div(cache->n_heads);
+    p.heads_div = fast_div(n_heads);
+    p.causal = causal != 0;
+    return p;
 }
 
 int check_state(const lora_kv_state *s)
@@ -261,30 +306,83 @@ int lora_kv_attention(const lora_kv_cache *cache, int layer, const lora_kv_batch
     if (batch->n_rows == 0) return LORA_OK;
     if ((int64_t)batch->n_rows * n_heads > (1 << 29)) return LORA_ERR_TOO_LARGE;
     const int64_t width = (int64_t)n_heads * cache->head_dim;
-    if ((rc = check_rows(q, ldq, width)) != LORA_OK) return rc;
-    if ((rc = check_rows(out, ldo, width)) != LORA_OK) return rc;
-    if (q == out || !ws) return LORA_ERR_INVALID_ARG;
-    if (!aligned(ws, 16) || !aligned(lse, 4)) return LORA_ERR_MISALIGNED;
+    if ((rc = check_attention(q, ldq, out, ldo, lse, width, ws)) != LORA_OK) return rc;
     if (ws_bytes < lora_kv_attention_ws_bytes(cache, batch, n_heads)) return LORA_ERR_BUFFER_TOO_SMALL;
-    AttnParams p;
-    memset(&p, 0, sizeof p);
-    p.c = view_of(cache, layer);
-    p.b = rows_of(batch, cache->page_size);
-    p.q = static_cast<const uint16_t *>(q);
-    p.out = static_cast<uint16_t *>(out);
-    p.lse = lse;
-    p.ldq = ldq;
-    p.ldo = ldo;
-    // below infinity: equal scores stay equal, and all others are further apart than any weight shows
-    p.scale_log2 = (float)std::min(scale * 1.4426950408889634, (double)std::numeric_limits<float>::max());
-    p.heads = n_heads;
-    p.group = n_heads / cache->n_heads;
-    p.group_div = fast_div(p.group);
-    p.kv_div = fast_div(cache->n_heads);
-    p.heads_div = fast_div(n_heads);
-    p.causal = causal != 0;
+    AttnParams p = attention_params(cache, layer, batch, q, ldq, n_heads, out, ldo, lse, scale, causal);
     p.window = window < p.b.tokens_max ? window : 0;     // as wide as the longest sequence: no window
     LORA_HIP(launch_attention(p, batch->max_rows, ws, static_cast<hipStream_t>(stream)));
+    return LORA_OK;
+}
+
+size_t lora_kv_share_ws_bytes(int n_seqs)
+{
+    return n_seqs < 1 || n_seqs > LORA_MAX_ROWS_LONG ? 0 : share_ws_bytes(n_seqs);
+}
+
+int lora_kv_share(const lora_kv_cache *cache, const lora_kv_batch *batch, const lora_kv_shared *shared, int min_pages, int max_rows,
+                  void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != LORA_OK) return rc;
+    if ((rc = check_batch(batch, true)) != LORA_OK) return rc;
+    if ((rc = check_shared(shared, batch)) != LORA_OK) return rc;
+    if (min_pages < 1 || max_rows < 0) return LORA_ERR_INVALID_ARG;
+    if (batch->n_rows == 0) return LORA_OK;
+    if (!shared->ws) return LORA_ERR_INVALID_ARG;
+    if (!aligned(shared->ws, 16)) return LORA_ERR_MISALIGNED;
+    const int64_t rows = max_rows ? std::min<int64_t>(batch->n_rows, (int64_t)batch->n_seqs * max_rows) : batch->n_rows;
+    if (shared->n_rows < rows || shared->ws_bytes < share_ws_bytes(batch->n_seqs)) return LORA_ERR_BUFFER_TOO_SMALL;
+    ShareParams p;
+    memset(&p, 0, sizeof p);
+    p.b = rows_of(batch, cache->page_size);
+    p.groups = shared->groups;
+    p.rows = shared->rows;
+    p.own = shared->own;
+    p.place = shared->place;
+    p.counts = shared->counts;
+    p.ws = static_cast<int32_t *>(shared->ws);
+    p.page_shift = log2_of(cache->page_size);
+    p.min_pages = min_pages;
+    p.max_rows = max_rows ? max_rows : INT_MAX;
+    p.most = groups_of(shared->n_seqs);
+    p.most_rows = shared->n_rows;
+    LORA_HIP(launch_share(p, static_cast<hipStream_t>(stream)));
+    return LORA_OK;
+}
+
+size_t lora_kv_attention_shared_ws_bytes(const lora_kv_cache *cache, const lora_kv_batch *batch, const lora_kv_shared *shared, int n_heads)
+{
+    if (lora_kv_attention_ws_bytes(cache, batch, n_heads) == 0 || !shared || shared->n_rows < 0 || shared->n_rows > LORA_MAX_ROWS_LONG ||
+        shared->max_group_rows < 0 || std::max(batch->n_rows, shared->n_rows) * (int64_t)n_heads > kSharedRowsHeads)
+        return 0;
+    return attention_shared_ws_bytes(batch->n_seqs, batch->n_rows, batch->max_rows, shared->n_rows, shared->max_group_rows, n_heads,
+                                     cache->n_heads, cache->head_dim);
+}
+
+int lora_kv_attention_shared(const lora_kv_cache *cache, int layer, const lora_kv_batch *batch, const lora_kv_shared *shared,
+                             const void *q, int64_t ldq, int n_heads, void *out, int64_t ldo, float *lse, float scale, int causal,
+                             void *ws, size_t ws_bytes, void *stream)
+{
+    int rc = check_cache(cache);
+    if (rc != LORA_OK) return rc;
+    if (layer < 0 || layer >= cache->n_layers) return LORA_ERR_BAD_SHAPE;
+    if ((rc = check_batch(batch, true)) != LORA_OK) return rc;
+    if ((rc = check_shared(shared, batch)) != LORA_OK) return rc;
+    if (n_heads < 1 || n_heads % cache->n_heads || n_heads / cache->n_heads > LORA_KV_MAX_GROUP) return LORA_ERR_BAD_SHAPE;
+    if (!std::isfinite(scale) || scale <= 0.f) return LORA_ERR_INVALID_ARG;
+    if (batch->n_rows == 0) return LORA_OK;
+    if (std::max(batch->n_rows, shared->n_rows) * (int64_t)n_heads > kSharedRowsHeads) return LORA_ERR_TOO_LARGE;
+    if ((rc = check_attention(q, ldq, out, ldo, lse, (int64_t)n_heads * cache->head_dim, ws)) != LORA_OK) return rc;
+    if (ws_bytes < lora_kv_attention_shared_ws_bytes(cache, batch, shared, n_heads)) return LORA_ERR_BUFFER_TOO_SMALL;
+    AttnParams p = attention_params(cache, layer, batch, q, ldq, n_heads, out, ldo, lse, scale, causal);
+    p.g.groups = shared->groups;
+    p.g.rows = shared->rows;
+    p.g.own = shared->own;
+    p.g.place = shared->place;
+    p.g.counts = shared->counts;
+    p.g.most = groups_of(shared->n_seqs);
+    p.g.most_rows = shared->n_rows;
+    LORA_HIP(launch_attention_shared(p, batch->max_rows, shared->max_group_rows, ws, static_cast<hipStream_t>(stream)));
     return LORA_OK;
 }
 

@@ -9,6 +9,10 @@
 // lie across the end of a stretch leave partial results, two at most per workgroup, which join_kernel joins.
 //
 // Long tiles are work items of their own; where there are few, their tokens are cut evenly into several items.
+//
+// S: the batch's sequences share tokens (lora_kv_attention_shared).  The plan's sequences are then the groups first, whose rows are
+// those of their members and whose tokens are the shared ones, and behind them the batch's own, from the first token that their group
+// does not have.  Results of rows of groups go to whole_o and whole_ml, where merge_kernel finds both parts of a row.
 #pragma once
 #include "kv_device.h"
 #include "kv_work.h"
@@ -22,23 +26,80 @@ enum Kind { kShort, kLong };
 // The plan: a head of kPlanHead words, then kPlanArrays arrays over the sequences: units of short tiles before each
 // sequence, work items and partial results of long tiles, and rows x heads of long tiles to join; then the sequences
 // themselves.
-enum { kUnits, kShare, kUnitTokens, kChunk, kItems, kJoinUnits, kHeadWords };
-enum { kBaseUnit, kBaseItem, kBaseSlot, kBaseJoin, kPlanSums, kSeqRow0 = kPlanSums, kSeqRows, kSeqLen, kSeqArrays };
-static_assert(kHeadWords <= kPlanHead && kSeqArrays == kPlanArrays, "as many words as the host makes room for");
-constexpr int kInlineWords = kPlanHead + kPlanArrays * kInlineSeqs;
+enum { kUnits, kShare, kUnitTokens, kChunk, kItems, kJoinUnits, kGroupRows, kHeadWords };
+enum { kBaseUnit, kBaseItem, kBaseSlot, kBaseJoin, kPlanSums, kSeqRow0 = kPlanSums, kSeqRows, kSeqLen, kSeqArrays, kSeqFirst = kSeqArrays };
+static_assert(kHeadWords <= kPlanHead && kSeqArrays == kPlanArrays && kSeqFirst + 1 == kSharedArrays, "as many words as the host makes room for");
+
+// Sequences of the plan, those up to which it is made in LDS, and its arrays.
+template <bool S>
+__device__ inline int plan_seqs(const AttnParams &p) { return S ? p.g.most + p.b.n_seqs : p.b.n_seqs; }
+template <bool S>
+constexpr int kMostInline = S ? kSharedInline : kInlineSeqs;
+template <bool S>
+constexpr int kArrays = S ? kSharedArrays : kPlanArrays;
+template <bool S>
+constexpr int kInlineWords = kPlanHead + kArrays<S> * kMostInline<S>;
 
 struct Seq {
     int row0, rows, len, pos0;           // first new row and their number, length, position of the first new row
+    int first;                           // first token, 0 where nothing is shared
+    bool group;                          // of rows that share tokens; row0 counts in the list of such rows then
 };
 
-__device__ inline Seq seq_of(const KvRows &b, int s)
+// Where the rows of sequence s are in the list of groups' rows, -1 if in no group.
+__device__ inline int place_in_groups(const AttnParams &p, int s, int rows)
 {
+    const int at = p.g.place[s];
+    return at >= 0 && at <= p.g.most_rows - rows && p.g.own[s] > 0 ? at : -1;
+}
+
+template <bool S>
+__device__ inline Seq seq_of(const AttnParams &p, int s)
+{
+    const KvRows &b = p.b;
     Seq q;
+    q.group = S && s < p.g.most;
+    if (q.group) {
+        const int32_t *g = p.g.groups + 4 * (int64_t)s;
+        q.row0 = min(max(0, g[2]), p.g.most_rows);
+        q.rows = (unsigned)g[0] < (unsigned)b.n_seqs ? min(max(0, g[3]), p.g.most_rows - q.row0) : 0;
+        q.len = min(max(0, g[1]), b.tokens_max);
+        q.pos0 = q.len;                   // every row sees all of them
+        q.first = 0;
+        return q;
+    }
+    if (S) s -= p.g.most;
     q.row0 = min(max(0, b.row_start[s]), b.n_rows);
     q.rows = max(0, min(b.row_start[s + 1], b.n_rows) - q.row0);
     q.len = min(max(0, b.seq_len[s]), b.tokens_max);
     q.pos0 = q.len - q.rows;
+    q.first = S && place_in_groups(p, s, q.rows) >= 0 ? min(p.g.own[s], max(0, q.pos0)) : 0;
     return q;
+}
+
+// The slot whose table a sequence of the plan reads.
+template <bool S>
+__device__ inline int slot_of(const AttnParams &p, int s)
+{
+    if (!S) return s;
+    return uniform(s < p.g.most ? min((unsigned)p.g.groups[4 * (int64_t)s], (unsigned)p.b.n_seqs - 1u) : s - p.g.most);
+}
+
+// The batch's row of the plan's row `at` of such a sequence.
+template <bool S>
+__device__ inline int row_at(const AttnParams &p, const Seq &q, int at)
+{
+    return S && q.group ? (int)min((unsigned)p.g.rows[at], (unsigned)p.b.n_rows - 1u) : at;
+}
+
+// Where a finished row goes: its place in whole_o (by heads), or -1 for the output itself.
+template <bool S>
+__device__ inline int64_t whole_at(const AttnParams &p, const Seq &q, int s, int i)
+{
+    if (!S) return -1;
+    if (q.group) return q.row0 + i;
+    const int at = place_in_groups(p, s - p.g.most, q.rows);
+    return at < 0 ? -1 : (int64_t)p.g.most_rows + at + i;
 }
 
 template <Kind K>
@@ -49,7 +110,7 @@ template <Kind K>
 __device__ inline int tiles_of(const AttnParams &p, const Seq &q)
 {
     const int n = q.rows * p.group;
-    if ((n <= p.short_limit) != (K == kShort)) return 0;
+    if ((n <= (q.group ? p.group_limit : p.short_limit)) != (K == kShort)) return 0;
     return K == kShort ? (n + (1 << p.short_shift) - 1) >> p.short_shift : (n + kLongTile - 1) / kLongTile;
 }
 
@@ -57,7 +118,7 @@ __device__ inline int tiles_of(const AttnParams &p, const Seq &q)
 template <Kind K>
 __device__ inline int reach_of(const AttnParams &p, const Seq &q)
 {
-    if (!p.window) return q.len;
+    if (!p.window) return q.len - q.first;
     const int most = p.window - 1 + min(q.rows, tile_rows<K>(p) / p.group_div + 2);
     return min(q.len, most);
 }
@@ -86,7 +147,7 @@ __device__ inline Range range_of(const AttnParams &p, const Seq &q, int tile)
     const int i0 = tile * R / p.group_div, i1 = min(q.rows - 1, (tile * R + R - 1) / p.group_div);
     Range r;
     r.hi = p.causal ? max(0, min(q.len, q.pos0 + i1 + 1)) : q.len;
-    r.lo = p.window ? max(0, q.pos0 + i0 - p.window + 1) : 0;
+    r.lo = p.window ? max(0, q.pos0 + i0 - p.window + 1) : q.first;
     if (r.lo >= r.hi) r.lo = r.hi = 0;
     return r;
 }
@@ -127,20 +188,32 @@ __device__ inline void plan_head(const AttnParams &p, int32_t *plan, int shift, 
     plan[kJoinUnits] = sum[kBaseJoin];
 }
 
+// Rows that merge_kernel finishes; none where the batch's rows are no partition, as nothing is written then.
+__device__ inline int group_rows(const AttnParams &p, bool no_rows)
+{
+    return no_rows ? 0 : min(max(0, p.g.counts[1]), p.g.most_rows);
+}
+
+template <bool S>
 __device__ inline void store_seq(int32_t *plan, int64_t n_seqs, int s, const Seq &q)
 {
+    if (S) plan[kPlanHead + kSeqFirst * n_seqs + s] = q.first;
     plan[kPlanHead + kSeqRow0 * n_seqs + s] = q.row0;
     plan[kPlanHead + kSeqRows * n_seqs + s] = q.rows;
     plan[kPlanHead + kSeqLen * n_seqs + s] = q.len;
 }
 
-__device__ inline Seq planned_seq(const int32_t *plan, int64_t n_seqs, int s)
+template <bool S>
+__device__ inline Seq planned_seq(const AttnParams &p, const int32_t *plan, int s)
 {
+    const int64_t n_seqs = plan_seqs<S>(p);
     Seq q;
     q.row0 = uniform(plan[kPlanHead + kSeqRow0 * n_seqs + s]);
     q.rows = uniform(plan[kPlanHead + kSeqRows * n_seqs + s]);
     q.len = uniform(plan[kPlanHead + kSeqLen * n_seqs + s]);
-    q.pos0 = q.len - q.rows;
+    q.group = S && s < p.g.most;
+    q.first = S ? uniform(plan[kPlanHead + kSeqFirst * n_seqs + s]) : 0;
+    q.pos0 = q.group ? q.len : q.len - q.rows;
     return q;
 }
 
@@ -153,21 +226,30 @@ __device__ inline unsigned faults_of(const KvRows &b, int s)
     return bad;
 }
 
-// The plan of up to kInlineSeqs sequences, by one wave: lane l takes the sequences l * each .. of the batch.
+// The same of a sequence of the plan.
+template <bool S>
+__device__ inline unsigned plan_faults_of(const AttnParams &p, int s)
+{
+    if (!S) return faults_of(p.b, s);
+    return s < p.g.most ? 0u : faults_of(p.b, s - p.g.most);
+}
+
+// The plan of up to kMostInline sequences, by one wave: lane l takes the sequences l * each .. of the batch.
+template <bool S>
 __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
 {
-    constexpr int MOST = kInlineSeqs / 64;
-    const int lane = threadIdx.x & 63, n = p.b.n_seqs, each = (n + 63) >> 6;
+    constexpr int MOST = kMostInline<S> / 64;
+    const int lane = threadIdx.x & 63, n = plan_seqs<S>(p), each = (n + 63) >> 6;
     Seq q[MOST];
     unsigned bad = 0;
     float work = 0.f;
 #pragma unroll
     for (int k = 0; k < MOST; ++k) {
         const int s = lane * each + k;
-        q[k] = Seq{0, 0, 0, 0};
+        q[k] = Seq{0, 0, 0, 0, 0, false};
         if (k < each && s < n) {
-            q[k] = seq_of(p.b, s);
-            bad |= faults_of(p.b, s);
+            q[k] = seq_of<S>(p, s);
+            bad |= plan_faults_of<S>(p, s);
         }
     }
     float units = 0.f;
@@ -181,7 +263,8 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
         chunk = chunk_of(p, last_lane(wave_scan(work)));
     }
     int own[MOST][kPlanSums] = {}, sum[kPlanSums] = {};
-    if (!__any(bad & 2)) {                // rows that are no partition: no work at all
+    const bool no_rows = __any(bad & 2);
+    if (!no_rows) {                       // rows that are no partition: no work at all
 #pragma unroll
         for (int k = 0; k < MOST; ++k) {
             if (k >= each) break;
@@ -204,27 +287,30 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
     }
 #pragma unroll
     for (int k = 0; k < MOST; ++k)
-        if (k < each && lane * each + k < n) store_seq(plan, n, lane * each + k, q[k]);
+        if (k < each && lane * each + k < n) store_seq<S>(plan, n, lane * each + k, q[k]);
     if (lane == 63) plan_head(p, plan, shift, chunk, sum);
+    if (S && lane == 63) plan[kGroupRows] = group_rows(p, no_rows);
     if (bad && blockIdx.x == 0) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
 }
 
 // The plan: made in s_plan by the workgroup's first wave, or what plan_kernel has left in the workspace.  The first workgroup
 // leaves its own there for the launch after.
+template <bool S>
 __device__ inline const int32_t *plan_of(const AttnParams &p, int32_t *s_plan)
 {
-    if (p.b.n_seqs > kInlineSeqs) return p.plan;
-    if (threadIdx.x < 64) make_plan(p, s_plan);
+    if (plan_seqs<S>(p) > kMostInline<S>) return p.plan;
+    if (threadIdx.x < 64) make_plan<S>(p, s_plan);
     __syncthreads();
     if (blockIdx.x == 0)
-        for (int i = threadIdx.x; i < kPlanHead + kPlanArrays * p.b.n_seqs; i += blockDim.x) p.plan[i] = s_plan[i];
+        for (int i = threadIdx.x; i < kPlanHead + kArrays<S> * plan_seqs<S>(p); i += blockDim.x) p.plan[i] = s_plan[i];
     return s_plan;
 }
 
 // The sequence that entry n of one of the plan's arrays belongs to.
+template <bool S>
 __device__ inline int seq_at(const AttnParams &p, const int32_t *base, int n)
 {
-    return __builtin_amdgcn_readfirstlane(p.b.n_seqs == 1 ? 0 : wave_find(base, p.b.n_seqs, n));
+    return __builtin_amdgcn_readfirstlane(plan_seqs<S>(p) == 1 ? 0 : wave_find(base, plan_seqs<S>(p), n));
 }
 
 // A tile on the line of units.
@@ -232,12 +318,13 @@ struct Place {
     int s, head, tile, start, units;     // start: the tile's first unit on the line
 };
 
+template <bool S>
 __device__ inline Place place_of(const AttnParams &p, const int32_t *plan, int unit, Seq &q)
 {
-    const int32_t *base = plan + kPlanHead + kBaseUnit * p.b.n_seqs;
+    const int32_t *base = plan + kPlanHead + kBaseUnit * plan_seqs<S>(p);
     Place x;
-    x.s = seq_at(p, base, unit);
-    q = planned_seq(plan, p.b.n_seqs, x.s);
+    x.s = seq_at<S>(p, base, unit);
+    q = planned_seq<S>(p, plan, x.s);
     x.units = units_of(reach_of<kShort>(p, q), uniform(plan[kUnitTokens]));
     const int before = uniform(base[x.s]);
     const int pair = x.units == 1 ? unit - before : (unit - before) / x.units;
@@ -291,5 +378,6 @@ __device__ inline u32x2 read_transposed(const uint16_t *at)
 }
 
 hipError_t launch_attend_long(const AttnParams &p, int max_items, hipStream_t s);
+hipError_t launch_attend_long_shared(const AttnParams &p, int max_items, hipStream_t s);
 
 }  // namespace lora

@@ -31,18 +31,19 @@ constexpr int kPlanThreads = 1024;
 
 __device__ __align__(16) const unsigned zeros[4] = {0u, 0u, 0u, 0u};
 
-// The plan of batches of more than kInlineSeqs sequences: as make_plan, by a whole workgroup in rounds.
+// The plan of batches of more than kMostInline sequences: as make_plan, by a whole workgroup in rounds.
+template <bool S>
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
 {
     constexpr int WAVES = kPlanThreads / 64;
     __shared__ float s_work[WAVES], s_units[WAVES];
     __shared__ int s_sum[kPlanSums][WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = p.b.n_seqs;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = plan_seqs<S>(p);
     float work = 0.f, units = 0.f;
     unsigned bad = 0;
     for (int s = tid; s < n; s += kPlanThreads) {
-        const Seq q = seq_of(p.b, s);
-        bad |= faults_of(p.b, s);
+        const Seq q = seq_of<S>(p, s);
+        bad |= plan_faults_of<S>(p, s);
         work += (float)tiles_of<kLong>(p, q) * (float)reach_of<kLong>(p, q);
         units += (float)(tiles_of<kShort>(p, q) * p.c.n_heads) * (float)units_of(reach_of<kShort>(p, q), kUnitShift);
     }
@@ -60,9 +61,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
         const int s = s0 + tid;
         int own[kPlanSums] = {}, upto[kPlanSums];
         if (s < n) {
-            const Seq q = seq_of(p.b, s);
+            const Seq q = seq_of<S>(p, s);
             if (!no_rows) plan_entry(p, q, shift, chunk, own);
-            store_seq(p.plan, n, s, q);
+            store_seq<S>(p.plan, n, s, q);
         }
         __syncthreads();                  // the round before has been read
 #pragma unroll
@@ -83,6 +84,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
         }
     }
     if (tid == 0) plan_head(p, p.plan, shift, chunk, base);
+    if (S && tid == 0) p.plan[kGroupRows] = group_rows(p, no_rows);
 }
 
 // V^T of 16 columns and a block's 32 tokens, in the order of the second product (see above).
@@ -100,8 +102,8 @@ __device__ inline u32x4 v_tile(const uint16_t *s_v, int d)
 }
 
 // DP: width of a head rounded up to what the products take; FULL: it is the width itself, otherwise zeros stand beyond it.
-// MT: 16-row parts of a tile.  BLOCKS: workgroups of a CU.
-template <int DP, int MT, bool FULL, int BLOCKS>
+// MT: 16-row parts of a tile.  BLOCKS: workgroups of a CU.  S: sequences share tokens.
+template <int DP, int MT, bool FULL, int BLOCKS, bool S>
 __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams p)
 {
     constexpr int R = 16 * MT;
@@ -114,11 +116,11 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
     constexpr int kVBytes = kWaves * kBlock * DP * 2, kOBytes = kWaves * 16 * OS * 4;
     __shared__ __align__(16) char s_mem[kVBytes > kOBytes ? kVBytes : kOBytes];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-    __shared__ int32_t s_plan[kInlineWords];
+    __shared__ int32_t s_plan[kInlineWords<S>];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
-    const int32_t *plan = plan_of(p, s_plan);
+    const int32_t *plan = plan_of<S>(p, s_plan);
     const int D = FULL ? DP : p.c.dim;
     uint16_t *s_v = reinterpret_cast<uint16_t *>(s_mem) + wave * kBlock * DP;
     const unsigned v_lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)s_v;
@@ -140,12 +142,12 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
     bf16x8 qf[MT][KS];
     const auto take = [&](int u) {
         Seq q;
-        const Place pl = place_of(p, plan, u, q);
+        const Place pl = place_of<S>(p, plan, u, q);
         const int k0 = u - pl.start, k1 = min(pl.units, k0 + end - u), tile = pl.tile, head = pl.head;
         const Range rg = range_of<kShort>(p, q, tile);
         const int lo = rg.lo + (k0 << unit_shift), hi = k1 == pl.units ? rg.hi : min(rg.hi, rg.lo + (k1 << unit_shift));
         part = Part{q, pl.s, head, tile, lo, hi, k1 - k0, k1 - k0 == pl.units, u != first};
-        if (lo < hi) page = (p.b.table + (int64_t)pl.s * p.b.max_pages)[min(lo + wave * kBlock + (lane & 31), hi - 1) >> p.c.page_shift];
+        if (lo < hi) page = (p.b.table + (int64_t)slot_of<S>(p, pl.s) * p.b.max_pages)[min(lo + wave * kBlock + (lane & 31), hi - 1) >> p.c.page_shift];
         // this lane's rows
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -154,7 +156,7 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
             const bool real = r < q.rows * p.group;
             see_hi[mt] = !real ? 0 : p.causal ? min(hi, q.pos0 + i + 1) : hi;
             see_lo[mt] = p.window ? max(lo, q.pos0 + i - p.window + 1) : lo;
-            const uint16_t *from = p.q + (int64_t)(q.row0 + i) * p.ldq + (head * p.group + g) * D;
+            const uint16_t *from = p.q + (int64_t)(real ? row_at<S>(p, q, q.row0 + i) : 0) * p.ldq + (head * p.group + g) * D;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const int d = ks * 32 + grp * 8;
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[mt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        const int32_t *table = p.b.table + (int64_t)part.s * p.b.max_pages;
+        const int32_t *table = p.b.table + (int64_t)slot_of<S>(p, part.s) * p.b.max_pages;
         const uint16_t *kbase = p.c.k + head * p.c.head_stride, *vbase = p.c.v + head * p.c.head_stride;
 
         // lane l looks up the page of the block's token l % 32, a block ahead; tokens past the range are read as
@@ -329,28 +331,32 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
                     total += f[w] * s_l[w][row];
                 }
                 const int i = r / p.group_div;
-                const int64_t t = done.q.row0 + i;
+                const int64_t t = row_at<S>(p, done.q, done.q.row0 + i);
                 const int qh = head * p.group + r - i * p.group;
-                const int64_t at = slot * R + mt * 16 + row;
+                // parts of cut tiles and, where tokens are shared, of rows of groups
+                const int64_t both = done.whole ? whole_at<S>(p, done.q, done.s, i) : -1;
+                const bool final = done.whole && both < 0;
+                const int64_t at = both < 0 ? slot * R + mt * 16 + row : both * p.heads + qh;
+                float *part_o = both < 0 ? p.part_o : p.whole_o, *part_ml = both < 0 ? p.part_ml : p.whole_ml;
                 const float norm = total == 0.f ? 0.f : 1.f / total;
                 for (int d = (threadIdx.x & 15) * 4; d < D; d += 64) {
                     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int w = 0; w < kWaves; ++w)
                         sum += *reinterpret_cast<f32x4 *>(s_o + (w * 16 + row) * OS + d) * f[w];
-                    if (done.whole) {
+                    if (final) {
                         u32x2 b;
                         b[0] = pack_bf16_rne(sum[0] * norm, sum[1] * norm);
                         b[1] = pack_bf16_rne(sum[2] * norm, sum[3] * norm);
                         *reinterpret_cast<u32x2 *>(p.out + t * p.ldo + qh * D + d) = b;
                     } else {
-                        st16f(p.part_o + at * D + d, sum);
+                        st16f(part_o + at * D + d, sum);
                     }
                 }
                 if ((threadIdx.x & 15) == 0) {
-                    if (!done.whole) {
-                        p.part_ml[at * 2] = top;
-                        p.part_ml[at * 2 + 1] = total;
+                    if (!final) {
+                        part_ml[at * 2] = top;
+                        part_ml[at * 2 + 1] = total;
                     } else if (p.lse) {
                         p.lse[t * p.heads + qh] = total == 0.f ? -INFINITY : (ref * p.scale_log2 + __builtin_amdgcn_logf(total)) * kLn2;
                     }
@@ -364,8 +370,9 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
 // Adds up the parts of one row, by the rule of the running softmax: maxima and sums at ml[part(c) * 2], outputs at
 // po[part(c) * dim], for the parts c < n.  Lanes look at 64 parts' maxima and sums at a time, and hand their factors on to the
 // lanes that add up the outputs: DP / 4 lanes take one part's 16 bytes each, eight sets of parts are on their way at once.
+// whole: where the result goes in whole_o, or -1 for the output.
 template <int DP, class Part>
-__device__ inline void join_row(const AttnParams &p, const float *ml, const float *po, int n, Part part, int64_t t, int qh)
+__device__ inline void join_row(const AttnParams &p, const float *ml, const float *po, int n, Part part, int64_t t, int qh, int64_t whole)
 {
     constexpr int LANES = DP / 4, SETS = 64 / LANES, DEEP = 8;
     const int lane = threadIdx.x & 63, set = lane / LANES, d = (lane % LANES) * 4, D = p.c.dim;
@@ -402,6 +409,12 @@ __device__ inline void join_row(const AttnParams &p, const float *ml, const floa
     for (int x = LANES; x < 64; x <<= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], x);
+    if (whole >= 0) {
+        const int64_t at = whole * p.heads + qh;
+        if (set == 0 && d < D) st16f(p.whole_o + at * D + d, sum);
+        if (lane == 0) p.whole_ml[at * 2] = m, p.whole_ml[at * 2 + 1] = total;
+        return;
+    }
     const float norm = total == 0.f ? 0.f : 1.f / total;
     if (set == 0 && d < D) {
         u32x2 b;
@@ -417,7 +430,7 @@ __device__ inline void join_row(const AttnParams &p, const float *ml, const floa
 
 // Joins the parts of short tiles that lie across the ends of workgroups' stretches: a workgroup per such end, the first
 // one inside a tile does it.  Workgroups from short_blocks on: the rows of cut long tiles, a wave per row and head.
-template <int DP>
+template <int DP, bool S>
 __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
 {
     const int32_t *plan = p.plan;        // the kernels before have left it
@@ -426,7 +439,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         const int share = uniform(plan[kShare]), b = blockIdx.x, cut = (b + 1) * share;
         if (cut >= plan[kUnits]) return;
         Seq q;
-        const Place pl = place_of(p, plan, cut, q);
+        const Place pl = place_of<S>(p, plan, cut, q);
         if (pl.start == cut || pl.start < b * share) return;       // between two tiles, or not the first end inside this one
         const int n = (pl.start + pl.units - 1) / share - b + 1;
         const int rows = min(1 << p.short_shift, q.rows * p.group - (pl.tile << p.short_shift));
@@ -434,16 +447,18 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
             const int r = (pl.tile << p.short_shift) + row, i = r / p.group_div;
             // the part of workgroup b + c: its last tile if it starts before, else its first
             const auto part = [&](int c) { return (((int64_t)2 * (b + c) + (c == 0 && pl.start != b * share)) << p.short_shift) + row; };
-            join_row<DP>(p, p.part_ml, p.part_o, n, part, q.row0 + i, pl.head * p.group + r - i * p.group);
+            join_row<DP>(p, p.part_ml, p.part_o, n, part, row_at<S>(p, q, q.row0 + i), pl.head * p.group + r - i * p.group,
+                         whole_at<S>(p, q, pl.s, i));
         }
         return;
     }
-    const int32_t *base = plan + kPlanHead + kBaseJoin * p.b.n_seqs, *slots = plan + kPlanHead + kBaseSlot * p.b.n_seqs;
+    const int seqs = plan_seqs<S>(p);
+    const int32_t *base = plan + kPlanHead + kBaseJoin * seqs, *slots = plan + kPlanHead + kBaseSlot * seqs;
     if (blockIdx.y) return;
     const int units = plan[kJoinUnits], chunk = plan[kChunk];
     for (int u = (blockIdx.x - p.join_blocks) * 4 + wave; u < units; u += (gridDim.x - p.join_blocks) * 4) {
-        const int s = seq_at(p, base, u);
-        const Seq q = planned_seq(plan, p.b.n_seqs, s);
+        const int s = seq_at<S>(p, base, u);
+        const Seq q = planned_seq<S>(p, plan, s);
         const int left = u - base[s];
         const int i = left / p.heads_div, qh = left - i * p.heads;
         const int head = qh / p.group_div;
@@ -453,15 +468,97 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         if (cuts == 1) continue;
         const int slot = slots[s] + tile * splits_of(reach_of<kLong>(p, q), chunk) * p.c.n_heads + head;
         const auto part = [&](int c) { return (int64_t)(slot + c * p.c.n_heads) * kLongTile + r - tile * kLongTile; };
-        join_row<DP>(p, p.long_ml, p.long_o, cuts, part, q.row0 + i, qh);
+        join_row<DP>(p, p.long_ml, p.long_o, cuts, part, row_at<S>(p, q, q.row0 + i), qh, whole_at<S>(p, q, s, i));
     }
 }
 
-template <int DP, int MT, int BLOCKS>
+// Puts together the two parts of the rows of groups, over the shared tokens and over their own, by the rule of the running
+// softmax; a set of dim / 4 lanes per row and head.
+__global__ __launch_bounds__(256) void merge_kernel(AttnParams p)
+{
+    const int D = p.c.dim, lanes = D <= 64 ? 16 : D <= 128 ? 32 : 64, sets = 256 / lanes;
+    const int d = (threadIdx.x % lanes) * 4;
+    const int64_t n = (int64_t)p.plan[kGroupRows] * p.heads, second = (int64_t)p.g.most_rows * p.heads;
+    for (int64_t at = (int64_t)blockIdx.x * sets + threadIdx.x / lanes; at < n; at += (int64_t)gridDim.x * sets) {
+        const int v = (int)at / p.heads_div, qh = (int)at - v * p.heads;
+        const int t = min((unsigned)p.g.rows[v], (unsigned)p.b.n_rows - 1u);
+        const float m0 = p.whole_ml[at * 2], l0 = p.whole_ml[at * 2 + 1];
+        const float m1 = p.whole_ml[(second + at) * 2], l1 = p.whole_ml[(second + at) * 2 + 1];
+        const float m = fmaxf(m0, m1), ref = m == -INFINITY ? 0.f : m;
+        const float f0 = __builtin_amdgcn_exp2f((m0 - ref) * p.scale_log2), f1 = __builtin_amdgcn_exp2f((m1 - ref) * p.scale_log2);
+        const float total = f0 * l0 + f1 * l1;
+        const float norm = total == 0.f ? 0.f : 1.f / total;
+        if (d < D) {
+            const f32x4 o = ld16f(p.whole_o + at * D + d) * f0 + ld16f(p.whole_o + (second + at) * D + d) * f1;
+            u32x2 b;
+            b[0] = pack_bf16_rne(o[0] * norm, o[1] * norm);
+            b[1] = pack_bf16_rne(o[2] * norm, o[3] * norm);
+            *reinterpret_cast<u32x2 *>(p.out + (int64_t)t * p.ldo + qh * D + d) = b;
+        }
+        if (d == 0 && p.lse) p.lse[(int64_t)t * p.heads + qh] = total == 0.f ? -INFINITY : (ref * p.scale_log2 + __builtin_amdgcn_logf(total)) * kLn2;
+    }
+}
+
+template <int DP, int MT, int BLOCKS, bool S>
 void launch_attend(const AttnParams &p, unsigned grid, hipStream_t s)
 {
-    if (p.c.dim == DP) hipLaunchKernelGGL((attend_kernel<DP, MT, true, BLOCKS>), dim3(grid), dim3(kWaves * 64), 0, s, p);
-    else hipLaunchKernelGGL((attend_kernel<DP, MT, false, BLOCKS>), dim3(grid), dim3(kWaves * 64), 0, s, p);
+    if (p.c.dim == DP) hipLaunchKernelGGL((attend_kernel<DP, MT, true, BLOCKS, S>), dim3(grid), dim3(kWaves * 64), 0, s, p);
+    else hipLaunchKernelGGL((attend_kernel<DP, MT, false, BLOCKS, S>), dim3(grid), dim3(kWaves * 64), 0, s, p);
+}
+
+// Where the workspace has what, and which kernels run.
+void lay_out(AttnParams &p, const Kinds &k, const AttnWs &at, void *ws)
+{
+    char *w = static_cast<char *>(ws);
+    p.plan = reinterpret_cast<int32_t *>(w + at.plan);
+    p.part_ml = reinterpret_cast<float *>(w + at.short_ml);
+    p.part_o = reinterpret_cast<float *>(w + at.short_o);
+    p.long_ml = reinterpret_cast<float *>(w + at.long_ml);
+    p.long_o = k.has_long ? reinterpret_cast<float *>(w + at.long_o) : nullptr;
+    p.short_limit = k.limit;
+    p.short_shift = k.shift;
+    p.short_blocks = k.blocks;
+}
+
+// The kernels of short tiles and the join.  tiles: short tiles of a head, at most; join_rows: rows of a tile that join_kernel
+// takes side by side.
+template <bool S>
+hipError_t launch_short_and_join(AttnParams &p, const Kinds &k, int64_t reach, int64_t tiles, unsigned join_rows, hipStream_t s)
+{
+    unsigned grid = 0;
+    if (k.has_short) {
+        grid = (unsigned)std::min<int64_t>(k.blocks, tiles * p.c.n_heads * ((reach + (1 << kUnitShift) - 1) >> kUnitShift));
+        if (p.c.dim <= 64 && k.shift == 5) launch_attend<64, 2, 2, S>(p, grid, s);
+        else if (p.c.dim <= 64) launch_attend<64, 1, 3, S>(p, grid, s);
+        else if (p.c.dim <= 128 && k.shift == 5) launch_attend<128, 2, 2, S>(p, grid, s);
+        else if (p.c.dim <= 128) launch_attend<128, 1, 3, S>(p, grid, s);
+        else launch_attend<256, 1, 2, S>(p, grid, s);
+    }
+    // parts: of short tiles of more than one unit, of long ones that may be cut
+    const unsigned join_long = k.has_long && reach > kLongMinSplit ? 1024 : 0;
+    p.join_blocks = k.has_short && reach > 1 << kUnitShift ? (int)grid - 1 : 0;
+    if (p.join_blocks + join_long > 0) {
+        const dim3 both(p.join_blocks + join_long, (join_rows + 3) / 4), block(256);
+        if (p.c.dim <= 64) hipLaunchKernelGGL((join_kernel<64, S>), both, block, 0, s, p);
+        else if (p.c.dim <= 128) hipLaunchKernelGGL((join_kernel<128, S>), both, block, 0, s, p);
+        else hipLaunchKernelGGL((join_kernel<256, S>), both, block, 0, s, p);
+    }
+    return hipGetLastError();
+}
+
+struct SharedWs : AttnWs {
+    size_t whole_ml, whole_o;
+};
+
+SharedWs shared_ws_of(int n_seqs, int group_rows, const SharedKinds &k, int heads, int dim)
+{
+    SharedWs w;
+    static_cast<AttnWs &>(w) = attn_ws_of(groups_of(n_seqs) + n_seqs, k, dim, kSharedArrays);
+    const size_t rows = 2 * (size_t)group_rows * heads;
+    w.whole_ml = w.bytes;
+    w.whole_o = w.whole_ml + up256(rows * 8);
+    w.bytes = w.whole_o + up256(rows * dim * 4);
+    return w;
 }
 
 }  // namespace
@@ -474,43 +571,45 @@ size_t attention_ws_bytes(int n_seqs, int n_rows, int max_rows, int heads, int k
 hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s)
 {
     const Kinds k = kinds_of(p.b.n_seqs, p.b.n_rows, max_rows, p.heads, p.c.n_heads, p.c.dim);
-    const AttnWs at = attn_ws_of(p.b.n_seqs, k, p.c.dim);
-    char *w = static_cast<char *>(ws);
-    p.plan = reinterpret_cast<int32_t *>(w + at.plan);
-    p.part_ml = reinterpret_cast<float *>(w + at.short_ml);
-    p.part_o = reinterpret_cast<float *>(w + at.short_o);
-    p.long_ml = reinterpret_cast<float *>(w + at.long_ml);
-    p.long_o = k.has_long ? reinterpret_cast<float *>(w + at.long_o) : nullptr;
-    p.short_limit = k.limit;
-    p.short_shift = k.shift;
-    p.short_blocks = k.blocks;
-    if (p.b.n_seqs > kInlineSeqs) hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+    lay_out(p, k, attn_ws_of(p.b.n_seqs, k, p.c.dim), ws);
+    if (p.b.n_seqs > kInlineSeqs) hipLaunchKernelGGL(plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, p);
     if (k.has_long) {
         const hipError_t e = launch_attend_long(p, (int)k.long_items, s);
         if (e != hipSuccess) return e;
     }
     const int64_t reach = p.window ? std::min<int64_t>(p.b.tokens_max, (int64_t)p.window + kLongTile) : p.b.tokens_max;
-    unsigned grid = 0;
-    if (k.has_short) {
-        const int64_t tiles = std::min(p.b.n_seqs, p.b.n_rows) + ((int64_t)p.b.n_rows * p.group >> k.shift);
-        grid = (unsigned)std::min<int64_t>(k.blocks, tiles * p.c.n_heads * ((reach + (1 << kUnitShift) - 1) >> kUnitShift));
-        if (p.c.dim <= 64 && k.shift == 5) launch_attend<64, 2, 2>(p, grid, s);
-        else if (p.c.dim <= 64) launch_attend<64, 1, 3>(p, grid, s);
-        else if (p.c.dim <= 128 && k.shift == 5) launch_attend<128, 2, 2>(p, grid, s);
-        else if (p.c.dim <= 128) launch_attend<128, 1, 3>(p, grid, s);
-        else launch_attend<256, 1, 2>(p, grid, s);
+    const int64_t tiles = std::min(p.b.n_seqs, p.b.n_rows) + ((int64_t)p.b.n_rows * p.group >> k.shift);
+    // a wave per row of a tile, or per four rows where most sequences are likely to have one new row only
+    const unsigned rows = k.has_long ? 1 : (unsigned)std::min<int64_t>(1 << k.shift, (int64_t)(max_rows > 0 ? max_rows : p.b.n_rows) * p.group);
+    return launch_short_and_join<false>(p, k, reach, tiles, rows, s);
+}
+
+size_t attention_shared_ws_bytes(int n_seqs, int n_rows, int max_rows, int group_rows, int max_group_rows, int heads, int kv_heads, int dim)
+{
+    const SharedKinds k = shared_kinds_of(n_seqs, n_rows, max_rows, group_rows, max_group_rows, heads, kv_heads, dim);
+    return shared_ws_of(n_seqs, group_rows, k, heads, dim).bytes;
+}
+
+hipError_t launch_attention_shared(AttnParams &p, int max_rows, int max_group_rows, void *ws, hipStream_t s)
+{
+    const SharedKinds k = shared_kinds_of(p.b.n_seqs, p.b.n_rows, max_rows, p.g.most_rows, max_group_rows, p.heads, p.c.n_heads, p.c.dim);
+    const SharedWs at = shared_ws_of(p.b.n_seqs, p.g.most_rows, k, p.heads, p.c.dim);
+    lay_out(p, k, at, ws);
+    p.group_limit = k.group_limit;
+    p.whole_ml = reinterpret_cast<float *>(static_cast<char *>(ws) + at.whole_ml);
+    p.whole_o = reinterpret_cast<float *>(static_cast<char *>(ws) + at.whole_o);
+    if (p.g.most + p.b.n_seqs > kSharedInline) hipLaunchKernelGGL(plan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, s, p);
+    if (k.has_long) {
+        const hipError_t e = launch_attend_long_shared(p, (int)k.long_items, s);
+        if (e != hipSuccess) return e;
     }
-    // parts: of short tiles of more than one unit, of long ones that may be cut
-    const unsigned join_long = k.has_long && reach > kLongMinSplit ? 1024 : 0;
-    p.join_blocks = k.has_short && reach > 1 << kUnitShift ? (int)grid - 1 : 0;
-    if (p.join_blocks + join_long > 0) {
-        // a wave per row of a tile, or per four rows where most sequences are likely to have one new row only
-        const unsigned rows = k.has_long ? 1 : (unsigned)std::min<int64_t>(1 << k.shift, (int64_t)(max_rows > 0 ? max_rows : p.b.n_rows) * p.group);
-        const dim3 both(p.join_blocks + join_long, (rows + 3) / 4), block(256);
-        if (p.c.dim <= 64) hipLaunchKernelGGL(join_kernel<64>, both, block, 0, s, p);
-        else if (p.c.dim <= 128) hipLaunchKernelGGL(join_kernel<128>, both, block, 0, s, p);
-        else hipLaunchKernelGGL(join_kernel<256>, both, block, 0, s, p);
-    }
+    const int64_t rows = (int64_t)p.b.n_rows + p.g.most_rows;
+    const int64_t tiles = std::min(p.b.n_seqs, p.b.n_rows) + p.g.most + (rows * p.group >> k.shift);
+    const hipError_t e = launch_short_and_join<true>(p, k, p.b.tokens_max, tiles, 1 << k.shift, s);
+    if (e != hipSuccess) return e;
+    const int lanes = p.c.dim <= 64 ? 16 : p.c.dim <= 128 ? 32 : 64;
+    const int64_t blocks = ((int64_t)p.g.most_rows * p.heads * lanes + 255) / 256;
+    if (blocks) hipLaunchKernelGGL(merge_kernel, dim3((unsigned)std::min<int64_t>(blocks, 4096)), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 

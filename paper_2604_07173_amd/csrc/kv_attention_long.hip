@@ -63,7 +63,8 @@ __device__ inline int of_load(int x, int j)
 }
 
 // DP: width of a head rounded up.  FULL: it is the width itself; otherwise pieces beyond it are filled with zeros.
-template <int DP, bool FULL>
+// S: sequences share tokens.
+template <int DP, bool FULL, bool S>
 __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_kernel(AttnParams p)
 {
     constexpr int KS = DP / 16;          // steps of the first product
@@ -78,14 +79,14 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int D = FULL ? DP : p.c.dim;
-    __shared__ int32_t s_plan[kInlineWords];
-    const int32_t *plan = plan_of(p, s_plan);
+    __shared__ int32_t s_plan[kInlineWords<S>];
+    const int32_t *plan = plan_of<S>(p, s_plan);
     const int n = blockIdx.x;
     if (n >= plan[kItems]) return;
     // the cuts of a tile lie n_heads apart, tiles behind each other, those with the longest ranges first
-    const int32_t *base = plan + kPlanHead + kBaseItem * p.b.n_seqs;
-    const int seq = seq_at(p, base, n);
-    const Seq q = planned_seq(plan, p.b.n_seqs, seq);
+    const int32_t *base = plan + kPlanHead + kBaseItem * plan_seqs<S>(p);
+    const int seq = seq_at<S>(p, base, n);
+    const Seq q = planned_seq<S>(p, plan, seq);
     const int left = uniform(n - base[seq]);
     const int pair = left / p.kv_div, head = left - pair * p.c.n_heads;
     const int chunk = uniform(plan[kChunk]);
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     if (cut >= splits) return;
     const int each = cut_of(rg, splits);
     const int lo = rg.lo + cut * each, hi = min(rg.hi, lo + each);
-    const int slot = plan[kPlanHead + kBaseSlot * p.b.n_seqs + seq] + (tile * cuts + cut) * p.c.n_heads + head;
+    const int slot = plan[kPlanHead + kBaseSlot * plan_seqs<S>(p) + seq] + (tile * cuts + cut) * p.c.n_heads + head;
 
     // this lane's row, and the tokens that it, some row and every row of its wave see
     const int r0 = tile * kRows + wave * 32;
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     const int r = r0 + col;
     const int i = r / p.group_div, g = r - i * p.group;
     const bool real = r < n_rows;
-    const int64_t t = q.row0 + i;
+    const int64_t t = real ? row_at<S>(p, q, q.row0 + i) : 0;
     const int qh = head * p.group + g;
     const int see_hi = !real ? 0 : p.causal ? min(hi, q.pos0 + i + 1) : hi;
     const int see_lo = p.window ? max(lo, q.pos0 + i - p.window + 1) : lo;
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
 
     // This wave's loads of a step: load j covers rows (wave * NL + j) * RPL + lane / CH.  Lane j of every CH lanes looks up
     // the page of load j's row and hands the place to the others; a lane fetches the piece that belongs at its place.
-    const int32_t *table = p.b.table + (int64_t)seq * p.b.max_pages;
+    const int32_t *table = p.b.table + (int64_t)slot_of<S>(p, seq) * p.b.max_pages;
     const int place_mask = (1 << p.c.page_shift) - 1;
     const uint16_t *kbase = p.c.k + head * p.c.head_stride, *vbase = p.c.v + head * p.c.head_stride;
     const int my_row = (wave * NL + (lane & (NL - 1))) * RPL + lane / CH;
@@ -325,7 +326,8 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     l += other_half(l);
     if (!real) return;
     const float ref = ms == -INFINITY ? 0.f : ms;
-    if (splits == 1) {
+    const int64_t whole = splits == 1 ? whole_at<S>(p, q, seq, i) : -1;
+    if (splits == 1 && whole < 0) {
         const float norm = l == 0.f ? 0.f : 1.f / l;
         uint16_t *out = p.out + t * p.ldo + (int64_t)qh * D;
 #pragma unroll
@@ -341,29 +343,33 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
             }
         if (p.lse && half == 0) p.lse[t * p.heads + qh] = l == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l)) * kLn2;
     } else {
-        const int64_t at = (int64_t)slot * kRows + wave * 32 + col;
+        const int64_t at = whole < 0 ? (int64_t)slot * kRows + wave * 32 + col : whole * p.heads + qh;
+        float *part_o = whole < 0 ? p.long_o : p.whole_o, *part_ml = whole < 0 ? p.long_ml : p.whole_ml;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int c = d * 32 + e * 8 + half * 4;
-                if (c < D) st16f(p.long_o + at * D + c, f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]});
+                if (c < D) st16f(part_o + at * D + c, f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]});
             }
         if (half == 0) {
-            p.long_ml[at * 2] = m;
-            p.long_ml[at * 2 + 1] = l;
+            part_ml[at * 2] = m;
+            part_ml[at * 2 + 1] = l;
         }
     }
 }
 
 }  // namespace
 
-hipError_t launch_attend_long(const AttnParams &p, int max_items, hipStream_t s)
+namespace {
+
+template <bool S>
+hipError_t launch_long(const AttnParams &p, int max_items, hipStream_t s)
 {
     const dim3 grid(max_items), block(kWaves * 64);
-#define LORA_LONG(DP)                                                                                       \
-    if (p.c.dim == DP) hipLaunchKernelGGL((attend_long_kernel<DP, true>), grid, block, 0, s, p);            \
-    else if (p.c.dim < DP) hipLaunchKernelGGL((attend_long_kernel<DP, false>), grid, block, 0, s, p);
+#define LORA_LONG(DP)                                                                                          \
+    if (p.c.dim == DP) hipLaunchKernelGGL((attend_long_kernel<DP, true, S>), grid, block, 0, s, p);            \
+    else if (p.c.dim < DP) hipLaunchKernelGGL((attend_long_kernel<DP, false, S>), grid, block, 0, s, p);
     if (p.c.dim <= 64) {
         LORA_LONG(64)
     } else if (p.c.dim <= 128) {
@@ -374,5 +380,10 @@ hipError_t launch_attend_long(const AttnParams &p, int max_items, hipStream_t s)
 #undef LORA_LONG
     return hipGetLastError();
 }
+
+}  // namespace
+
+hipError_t launch_attend_long(const AttnParams &p, int max_items, hipStream_t s) { return launch_long<false>(p, max_items, s); }
+hipError_t launch_attend_long_shared(const AttnParams &p, int max_items, hipStream_t s) { return launch_long<true>(p, max_items, s); }
 
 }  // namespace lora

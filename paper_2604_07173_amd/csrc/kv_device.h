@@ -48,4 +48,29 @@ __device__ inline T last_lane(T x)
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
+// Inclusive prefix sum over a workgroup of WAVES waves; `total` comes back to every thread.
+template <int WAVES, class T>
+__device__ inline T block_scan(T v, T &total)
+{
+    __shared__ T s_sum[WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const T o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    __syncthreads();                      // a former call's sums have been read
+    if (lane == 63) s_sum[wave] = v;
+    __syncthreads();
+    T before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const T x = s_sum[w];
+        if (w < wave) before += x;
+        total += x;
+    }
+    return v + before;
+}
+
 }  // namespace lora

@@ -27,6 +27,12 @@ struct KvRows {
     int n_seqs, n_rows, max_pages, tokens_max;
 };
 
+// Groups of sequences that hold the same first pages, as lora_kv_shared says.  most: room for groups; most_rows: for their rows.
+struct KvGroups {
+    const int32_t *groups, *rows, *own, *place, *counts;
+    int most, most_rows;
+};
+
 struct AppendParams {
     KvView c;
     KvRows b;
@@ -56,6 +62,17 @@ struct AttnParams {
     int32_t *plan;                // device: see kv_attention.h
     float *part_o, *part_ml;      // partial results of short tiles whose range is cut: sums, and maximum and sum of weights
     float *long_o, *long_ml;
+    // lora_kv_attention_shared only
+    KvGroups g;
+    int group_limit;              // as short_limit, of a group's rows
+    float *whole_o, *whole_ml;    // of groups' rows and heads: over the shared tokens, then over their own
+};
+
+struct ShareParams {
+    KvRows b;
+    int32_t *groups, *rows, *own, *place, *counts;
+    int32_t *ws;
+    int page_shift, min_pages, max_rows, most, most_rows;
 };
 
 struct PlanParams {
@@ -80,6 +97,10 @@ struct CopyParams {
 hipError_t launch_append(const AppendParams &p, hipStream_t s);
 size_t attention_ws_bytes(int n_seqs, int n_rows, int max_rows, int heads, int kv_heads, int dim);
 hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s);
+size_t attention_shared_ws_bytes(int n_seqs, int n_rows, int max_rows, int group_rows, int max_group_rows, int heads, int kv_heads, int dim);
+hipError_t launch_attention_shared(AttnParams &p, int max_rows, int max_group_rows, void *ws, hipStream_t s);
+size_t share_ws_bytes(int n_seqs);
+hipError_t launch_share(const ShareParams &p, hipStream_t s);
 size_t plan_ws_bytes(int n_pages, int n_seqs);
 hipError_t launch_plan(const PlanParams &p, hipStream_t s);
 hipError_t launch_compact(const PlanParams &p, hipStream_t s);

@@ -29,6 +29,8 @@ constexpr int kShortEqual = 32, kShortLimit = 64;
 constexpr int kInlineSeqs = 256;         // sequences up to which every workgroup makes the plan for itself, in LDS: one launch less
 // 32-bit words of the plan in memory: of its head, and of each sequence
 constexpr int kPlanHead = 8, kPlanArrays = 7;
+// the same for batches that share tokens: groups and sequences, with the tokens that each begins at
+constexpr int kSharedInline = kInlineSeqs + kInlineSeqs / 2, kSharedArrays = 8;
 
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -66,16 +68,46 @@ inline Kinds kinds_of(int n_seqs, int n_rows, int max_rows, int heads, int kv_he
     return k;
 }
 
+// Room for groups of two sequences or more, of a batch of n_seqs.
+inline int groups_of(int n_seqs) { return n_seqs > 1 ? n_seqs / 2 : 1; }
+
+// The same where sequences share tokens (lora_kv_attention_shared): the plan's sequences are the groups, with the rows of their
+// members over the shared tokens, and behind them the batch's own, over the rest.
+struct SharedKinds : Kinds {
+    int group_limit;                      // as limit, of a group
+};
+
+constexpr int64_t kSharedRowsHeads = 1 << 26;      // rows x heads of such a batch: its long tiles, of 17 rows or more, make no grid too large
+constexpr int kGroupShort = 16;          // rows x group up to which a group goes in short tiles
+
+inline SharedKinds shared_kinds_of(int n_seqs, int n_rows, int max_rows, int group_rows, int max_group_rows, int heads, int kv_heads, int dim)
+{
+    const int64_t group = heads / kv_heads;
+    const int64_t most = max_rows > 0 ? std::min(max_rows, n_rows) : n_rows;
+    const int64_t most_group = max_group_rows > 0 ? std::min(max_group_rows, group_rows) : group_rows;
+    SharedKinds k;
+    k.has_short = true;
+    k.has_long = most * group > kShortLimit || most_group * group > kGroupShort;
+    k.limit = k.has_long ? kShortLimit : INT_MAX;
+    k.group_limit = k.has_long ? kGroupShort : INT_MAX;
+    const int64_t seqs = std::min<int64_t>(n_seqs, n_rows * group / (kShortLimit + 1));
+    const int64_t groups = std::min<int64_t>(groups_of(n_seqs), group_rows * group / (kGroupShort + 1));
+    k.long_items = kLongTarget + kv_heads * (seqs + groups + (n_rows + (int64_t)group_rows) * group / kLongTile);
+    k.shift = !k.has_long && most * group > 16 && dim <= 128 ? 5 : 4;
+    k.blocks = dim <= 128 && k.shift == 4 ? kMostBlocks : kMostBlocks / 3 * 2;
+    return k;
+}
+
 struct AttnWs {
     size_t plan, short_ml, short_o, long_ml, long_o, bytes;
 };
 
-inline AttnWs attn_ws_of(int n_seqs, const Kinds &k, int dim)
+inline AttnWs attn_ws_of(int n_seqs, const Kinds &k, int dim, int arrays = kPlanArrays)
 {
     const size_t rows_s = k.has_short ? 2 * (size_t)k.blocks << k.shift : 0, rows_l = k.has_long ? 2 * (size_t)kLongTarget * kLongTile : 0;
     AttnWs w;
     w.plan = 0;
-    w.short_ml = up256((kPlanHead + kPlanArrays * (size_t)n_seqs) * 4);
+    w.short_ml = up256((kPlanHead + arrays * (size_t)n_seqs) * 4);
     w.short_o = w.short_ml + up256(rows_s * 8);
     w.long_ml = w.short_o + up256(rows_s * dim * 4);
     w.long_o = w.long_ml + up256(rows_l * 8);

@@ -30,6 +30,8 @@ struct Library {
     decltype(&lora_kv_plan) kv_plan;
     decltype(&lora_kv_compact) kv_compact;
     decltype(&lora_kv_copy_pages) kv_copy_pages;
+    decltype(&lora_kv_share) kv_share;
+    decltype(&lora_kv_attention_shared) kv_attention_shared;
 } lib;
 
 // Python-side helpers, set by bind(): the slow but always right way to a stream's handle, and, once
@@ -413,6 +415,44 @@ LORA_PY(kv_attention)
     LORA_CALL(lib.kv_attention(c, layer, b, q, ldq, heads, o, ldo, (float *)lse, (float)scale, causal, window, ws, bytes, st));
 }
 
+// cache, batch, shared, min_pages, max_rows, stream
+LORA_PY(kv_share)
+{
+    lora_kv_cache *c;
+    lora_kv_batch *b;
+    lora_kv_shared *sh;
+    Held c_ref, b_ref, s_ref;
+    int pages, rows;
+    void *st;
+    if (!n_args(n, 6) || !structure_or_none(a[0], c, c_ref, "lora_kv_cache") || !structure_or_none(a[1], b, b_ref, "lora_kv_batch") ||
+        !structure_or_none(a[2], sh, s_ref, "lora_kv_shared") || !to_int(a[3], pages) || !to_int(a[4], rows) || !stream_of(a[5], st))
+        return nullptr;
+    LORA_CALL(lib.kv_share(c, b, sh, pages, rows, st));
+}
+
+// cache, layer, batch, shared, q, ldq, n_heads, out, ldo, lse, scale, causal, ws, stream
+LORA_PY(kv_attention_shared)
+{
+    lora_kv_cache *c;
+    lora_kv_batch *b;
+    lora_kv_shared *sh;
+    Held c_ref, b_ref, s_ref;
+    int layer, heads;
+    void *q, *o, *lse, *ws, *st;
+    int64_t ldq, ldo;
+    size_t bytes;
+    if (!n_args(n, 14) || !structure_or_none(a[0], c, c_ref, "lora_kv_cache") || !to_int(a[1], layer) ||
+        !structure_or_none(a[2], b, b_ref, "lora_kv_batch") || !structure_or_none(a[3], sh, s_ref, "lora_kv_shared") || !addr(a[4], q) ||
+        !to_i64(a[5], ldq) || !to_int(a[6], heads) || !addr(a[7], o) || !to_i64(a[8], ldo) || !addr(a[9], lse) ||
+        !ws_of(a[12], Py_None, ws, bytes) || !stream_of(a[13], st))
+        return nullptr;
+    const double scale = PyFloat_AsDouble(a[10]);
+    if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    const int causal = PyObject_IsTrue(a[11]);
+    if (causal < 0) return nullptr;
+    LORA_CALL(lib.kv_attention_shared(c, layer, b, sh, q, ldq, heads, o, ldo, (float *)lse, (float)scale, causal, ws, bytes, st));
+}
+
 // cache, from, to, src, new_len, moves, stream
 LORA_PY(kv_plan)
 {
@@ -510,6 +550,18 @@ LORA_PY(bind_kv)
     Py_RETURN_NONE;
 }
 
+// bind_shared(addresses): the functions of sequences that share pages
+LORA_PY(bind_shared)
+{
+    if (!n_args(n, 1)) return nullptr;
+    const Wanted want[] = {
+        {"lora_kv_share", (void **)&lib.kv_share}, {"lora_kv_attention_shared", (void **)&lib.kv_attention_shared},
+    };
+    for (const auto &w : want)
+        if (!address_of(a[0], w.name, w.at)) return nullptr;
+    Py_RETURN_NONE;
+}
+
 // use_current_stream(current device, raw stream of a device): torch's calls, once it has initialised
 // the device
 LORA_PY(use_current_stream)
@@ -527,7 +579,8 @@ PyMethodDef methods[] = {
     LORA_METHOD(bind), LORA_METHOD(bind_kv), LORA_METHOD(use_current_stream), LORA_METHOD(build_segments), LORA_METHOD(apply),
     LORA_METHOD(apply_group), LORA_METHOD(build_apply_group), LORA_METHOD(moe_apply), LORA_METHOD(moe_build_apply),
     LORA_METHOD(moe_down_combine), LORA_METHOD(load_adapter_layer), LORA_METHOD(rope_append),
-    LORA_METHOD(kv_attention), LORA_METHOD(kv_plan), LORA_METHOD(kv_compact), LORA_METHOD(kv_copy_pages), {nullptr, nullptr, 0, nullptr}};
+    LORA_METHOD(kv_attention), LORA_METHOD(kv_plan), LORA_METHOD(kv_compact), LORA_METHOD(kv_copy_pages),
+    LORA_METHOD(bind_shared), LORA_METHOD(kv_share), LORA_METHOD(kv_attention_shared), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
