@@ -20,6 +20,7 @@ from .binding import (  # noqa: F401
     KvCache, KvBatch, KvState, KvMoves, Rope, lora_rope_freqs, lora_rope_append,
     lora_kv_attention_ws_bytes, lora_kv_attention, lora_kv_moves_ws_bytes, lora_kv_plan, lora_kv_compact, lora_kv_copy_pages,
     KvShared, lora_kv_share_ws_bytes, lora_kv_share, lora_kv_attention_shared_ws_bytes, lora_kv_attention_shared,
+    Norm, Rows8, lora_add_norm, Sampling, lora_sample, LORA_NORM_MAX_WIDTH, LORA_NORM_MAX_ROWS, LORA_SAMPLE_MAX_VOCAB,
     LORA_STATUS_BAD_PAGE, LORA_STATUS_BAD_LENGTH, LORA_STATUS_BAD_SEQ, LORA_STATUS_NO_PAGES, LORA_ROPE_HALF,
     LORA_ROPE_INTERLEAVED, LORA_ROPE_PLAIN, LORA_ROPE_LINEAR, LORA_ROPE_BASE, LORA_ROPE_PARTS, LORA_KV_MAX_HEAD_DIM,
     LORA_KV_MAX_PAGE, LORA_KV_MAX_PAGES, LORA_KV_MAX_GROUP,

@@ -21,6 +21,7 @@ LORA_STATUS_BAD_PAGE, LORA_STATUS_BAD_LENGTH, LORA_STATUS_BAD_SEQ, LORA_STATUS_N
 LORA_ROPE_HALF, LORA_ROPE_INTERLEAVED = 0, 1
 LORA_ROPE_PLAIN, LORA_ROPE_LINEAR, LORA_ROPE_BASE, LORA_ROPE_PARTS = 0, 1, 2, 3
 LORA_KV_MAX_HEAD_DIM, LORA_KV_MAX_PAGE, LORA_KV_MAX_PAGES, LORA_KV_MAX_GROUP = 256, 1024, 0x7FFFFC00, 64
+LORA_NORM_MAX_WIDTH, LORA_NORM_MAX_ROWS, LORA_SAMPLE_MAX_VOCAB = 65536, 1 << 24, 1 << 22
 
 EXPORTED_SYMBOLS = [
     "lora_strerror", "lora_last_hip_error", "lora_pool_bytes", "lora_register_pool",
@@ -33,6 +34,7 @@ EXPORTED_SYMBOLS = [
     "lora_rope_freqs", "lora_rope_append", "lora_kv_attention_ws_bytes", "lora_kv_attention", "lora_kv_moves_ws_bytes",
     "lora_kv_plan", "lora_kv_compact", "lora_kv_copy_pages",
     "lora_kv_share_ws_bytes", "lora_kv_share", "lora_kv_attention_shared_ws_bytes", "lora_kv_attention_shared",
+    "lora_add_norm", "lora_sample",
 ]
 
 
@@ -90,6 +92,19 @@ class _KvShared(C.Structure):
     _fields_ = [("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_group_rows", C.c_int32), ("reserved", C.c_int32),
                 ("groups", C.c_void_p), ("rows", C.c_void_p), ("own", C.c_void_p), ("place", C.c_void_p), ("counts", C.c_void_p),
                 ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("width", C.c_int32), ("weight_dtype", C.c_int32), ("eps", C.c_float), ("shift", C.c_float)]
+
+
+class _Rows8(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("scale", C.c_void_p), ("ld", C.c_int64), ("ld_scale", C.c_int64), ("group", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class _Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
 
 
 class _KvState(C.Structure):
@@ -240,6 +255,10 @@ def load_library():
     lib.lora_kv_compact.argtypes = [C.POINTER(_KvCache), C.POINTER(_KvState), C.POINTER(_KvState), C.POINTER(_KvMoves), vp]
     lib.lora_kv_copy_pages.restype = i32
     lib.lora_kv_copy_pages.argtypes = [C.POINTER(_KvCache), C.POINTER(_KvMoves), i32, vp]
+    lib.lora_add_norm.restype = i32
+    lib.lora_add_norm.argtypes = [C.POINTER(_Norm), i32, vp, i64, i32, vp, i64, i32, vp, i64, vp, i64, C.POINTER(_Rows8), vp]
+    lib.lora_sample.restype = i32
+    lib.lora_sample.argtypes = [vp, i64, i32, i32, i32, C.POINTER(_Sampling), vp, vp, vp, vp]
     global _pycall
     if not os.path.exists(os.path.join(os.path.dirname(path), "_pycall.so")):
         raise RuntimeError("_pycall.so is not built; run `python -m paper_2604_07173_amd.build`")
@@ -248,6 +267,7 @@ def load_library():
     calls.bind(addresses, _stream)
     calls.bind_kv(addresses)
     calls.bind_shared(addresses)
+    calls.bind_step(addresses)
     _pycall = calls
     _lib = lib
     return lib
@@ -784,6 +804,88 @@ def lora_kv_copy_pages(cache: KvCache, moves: KvMoves, max_moves: int, stream=No
     rc = _calls().kv_copy_pages(cache, moves, max_moves, stream)
     if rc:
         _check(rc, "lora_kv_copy_pages")
+
+
+# ---- between the blocks of a step (include/lora_step.h) ----------------------------------------
+
+
+def _dtype_of(t, what):
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float32) or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous bf16 or float32 tensor, got {t.dtype}")
+    return LORA_DTYPE_F32 if t.dtype == torch.float32 else LORA_DTYPE_BF16
+
+
+def _holds_floats(t, what, n):
+    """As _holds_int32, of float32."""
+    if hasattr(t, "is_contiguous") and (t.element_size() != 4 or not t.is_floating_point() or not t.is_contiguous() or t.numel() < n):
+        raise ValueError(f"{what}: a contiguous float32 tensor of {n} elements at least, got {t.dtype} {list(t.shape)}")
+
+
+class Norm:
+    """lora_norm over a weight tensor [width] (bf16 or float32), or without one.  Holds the tensor."""
+
+    def __init__(self, weight=None, eps: float = 1e-5, shift: float = 0.0, width: Optional[int] = None):
+        self.weight = weight
+        if weight is not None and weight.dim() != 1:
+            raise ValueError(f"weight: one dimension, got {list(weight.shape)}")
+        if weight is not None and width is not None and width != weight.numel():
+            raise ValueError(f"width: {weight.numel()} as the weight's, got {width}")
+        kind = LORA_DTYPE_BF16 if weight is None else _dtype_of(weight, "weight")
+        self.c = _Norm(_addr(weight), int(width or 0) if weight is None else weight.numel(), kind, eps, shift)
+
+
+class Rows8:
+    """lora_rows8 over values [rows][width] in 8 bits and scales [rows][groups] in float32, a scale for every `group` columns (0: one
+    for the row); rows may lie apart.  Holds the tensors."""
+
+    def __init__(self, values, scale, group: int = 0):
+        import torch
+        if values.element_size() != 1 or values.dim() != 2 or values.stride(1) != 1:
+            raise ValueError(f"values: [rows][width] in 8 bits, got {values.dtype} {list(values.shape)}")
+        groups = -(-values.shape[1] // group) if group > 0 else 1
+        if scale.dtype != torch.float32 or scale.dim() != 2 or scale.shape != (values.shape[0], groups) or (groups > 1 and scale.stride(1) != 1):
+            raise ValueError(f"scale: float32 {[values.shape[0], groups]}, got {scale.dtype} {list(scale.shape)}")
+        self.values, self.scale = values, scale
+        one = values.shape[0] <= 1                   # of one row the stride says nothing
+        self.c = _Rows8(values.data_ptr(), scale.data_ptr(), -(-values.shape[1] // 8) * 8 if one else values.stride(0),
+                        groups if one else scale.stride(0), group, 0)
+
+
+def lora_add_norm(norm: Norm, n_rows: int, x, ldx, add, ldadd, total, ldt, out, ldo, out8: Optional[Rows8] = None,
+                  x_dtype=LORA_DTYPE_BF16, add_dtype=LORA_DTYPE_BF16, stream=None):
+    """total, out, out8 (None if not wanted) from x + add: the sum, its norm in bf16 and in 8 bits."""
+    if isinstance(out8, Rows8) and isinstance(norm, Norm) and (out8.values.shape[0] < n_rows or out8.values.shape[1] != norm.c.width):
+        raise ValueError(f"out8: values of {n_rows} rows of {norm.c.width}, got {list(out8.values.shape)}")
+    rc = _calls().add_norm(norm, n_rows, x, ldx, x_dtype, add, ldadd, add_dtype, total, ldt, out, ldo, out8, stream)
+    if rc:
+        _check(rc, "lora_add_norm")
+
+
+class Sampling:
+    """lora_sampling over device tensors [rows] (float32, top_k int32), each None if not wanted.  Holds the tensors."""
+
+    def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
+        self.temperature, self.top_k, self.top_p, self.min_p = temperature, top_k, top_p, min_p
+        self.holds = 1 << 62                         # rows that all of them have room for
+        for t, what, holds in ((temperature, "temperature", _holds_floats), (top_k, "top_k", _holds_int32), (top_p, "top_p", _holds_floats),
+                               (min_p, "min_p", _holds_floats)):
+            if t is not None:
+                holds(t, what, 0)
+                self.holds = min(self.holds, t.numel())
+        self.c = _Sampling(_addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p))
+
+
+def lora_sample(logits, ld, n_rows: int, vocab: int, how: Sampling, u, token, prob=None, dtype=LORA_DTYPE_F32, stream=None):
+    if isinstance(how, Sampling) and how.holds < n_rows:
+        raise ValueError(f"how: settings of {n_rows} rows, got {how.holds}")
+    _holds_floats(u, "u", n_rows)
+    _holds_int32(token, "token", n_rows)
+    if prob is not None:
+        _holds_floats(prob, "prob", n_rows)
+    rc = _calls().sample(logits, ld, dtype, n_rows, vocab, how, u, token, prob, stream)
+    if rc:
+        _check(rc, "lora_sample")
 
 
 # ---- cache provisioning (include/lora_provision.h): host arrays in, numbers out ----------------

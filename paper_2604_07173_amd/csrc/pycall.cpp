@@ -13,6 +13,7 @@
 
 #include "../../include/lora.h"
 #include "../../include/lora_attn.h"
+#include "../../include/lora_step.h"
 
 namespace {
 
@@ -32,6 +33,8 @@ struct Library {
     decltype(&lora_kv_copy_pages) kv_copy_pages;
     decltype(&lora_kv_share) kv_share;
     decltype(&lora_kv_attention_shared) kv_attention_shared;
+    decltype(&lora_add_norm) add_norm;
+    decltype(&lora_sample) sample;
 } lib;
 
 // Python-side helpers, set by bind(): the slow but always right way to a stream's handle, and, once
@@ -453,6 +456,37 @@ LORA_PY(kv_attention_shared)
     LORA_CALL(lib.kv_attention_shared(c, layer, b, sh, q, ldq, heads, o, ldo, (float *)lse, (float)scale, causal, ws, bytes, st));
 }
 
+// norm, n_rows, x, ldx, x_dtype, add, ldadd, add_dtype, sum, ldsum, out, ldo, out8, stream
+LORA_PY(add_norm)
+{
+    lora_norm *w;
+    lora_rows8 *r8;
+    Held w_ref, r_ref;
+    int rows, xt, at;
+    void *x, *add, *sum, *out, *st;
+    int64_t ldx, lda, lds, ldo;
+    if (!n_args(n, 14) || !structure_or_none(a[0], w, w_ref, "lora_norm") || !to_int(a[1], rows) || !addr(a[2], x) || !to_i64(a[3], ldx) ||
+        !to_int(a[4], xt) || !addr(a[5], add) || !to_i64(a[6], lda) || !to_int(a[7], at) || !addr(a[8], sum) || !to_i64(a[9], lds) ||
+        !addr(a[10], out) || !to_i64(a[11], ldo) || !structure_or_none(a[12], r8, r_ref, "lora_rows8") || !stream_of(a[13], st))
+        return nullptr;
+    LORA_CALL(lib.add_norm(w, rows, x, ldx, xt, add, lda, at, sum, lds, out, ldo, r8, st));
+}
+
+// logits, ld, dtype, n_rows, vocab, how, u, token, prob, stream
+LORA_PY(sample)
+{
+    lora_sampling *how;
+    Held h_ref;
+    int type, rows, vocab;
+    void *x, *u, *token, *prob, *st;
+    int64_t ld;
+    if (!n_args(n, 10) || !addr(a[0], x) || !to_i64(a[1], ld) || !to_int(a[2], type) || !to_int(a[3], rows) || !to_int(a[4], vocab) ||
+        !structure_or_none(a[5], how, h_ref, "lora_sampling") || !addr(a[6], u) || !addr(a[7], token) || !addr(a[8], prob) ||
+        !stream_of(a[9], st))
+        return nullptr;
+    LORA_CALL(lib.sample(x, ld, type, rows, vocab, how, (const float *)u, (int32_t *)token, (float *)prob, st));
+}
+
 // cache, from, to, src, new_len, moves, stream
 LORA_PY(kv_plan)
 {
@@ -562,6 +596,18 @@ LORA_PY(bind_shared)
     Py_RETURN_NONE;
 }
 
+// bind_step(addresses): the functions between the blocks of a step
+LORA_PY(bind_step)
+{
+    if (!n_args(n, 1)) return nullptr;
+    const Wanted want[] = {
+        {"lora_add_norm", (void **)&lib.add_norm}, {"lora_sample", (void **)&lib.sample},
+    };
+    for (const auto &w : want)
+        if (!address_of(a[0], w.name, w.at)) return nullptr;
+    Py_RETURN_NONE;
+}
+
 // use_current_stream(current device, raw stream of a device): torch's calls, once it has initialised
 // the device
 LORA_PY(use_current_stream)
@@ -580,7 +626,8 @@ PyMethodDef methods[] = {
     LORA_METHOD(apply_group), LORA_METHOD(build_apply_group), LORA_METHOD(moe_apply), LORA_METHOD(moe_build_apply),
     LORA_METHOD(moe_down_combine), LORA_METHOD(load_adapter_layer), LORA_METHOD(rope_append),
     LORA_METHOD(kv_attention), LORA_METHOD(kv_plan), LORA_METHOD(kv_compact), LORA_METHOD(kv_copy_pages),
-    LORA_METHOD(bind_shared), LORA_METHOD(kv_share), LORA_METHOD(kv_attention_shared), {nullptr, nullptr, 0, nullptr}};
+    LORA_METHOD(bind_shared), LORA_METHOD(kv_share), LORA_METHOD(kv_attention_shared),
+    LORA_METHOD(bind_step), LORA_METHOD(add_norm), LORA_METHOD(sample), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
