@@ -12,7 +12,8 @@
 //
 // S: the batch's sequences share tokens (lora_kv_attention_shared).  The plan's sequences are then the groups first, whose rows are
 // those of their members and whose tokens are the shared ones, and behind them the batch's own, from the first token that their group
-// does not have.  Results of rows of groups go to whole_o and whole_ml, where merge_kernel finds both parts of a row.
+// does not have.  Results of rows of groups stay partial, and whoever begins a tile says where its rows' parts are (`found`): of tiles
+// that are not cut in whole_o and whole_ml.  join_kernel puts them together.
 #pragma once
 #include "kv_device.h"
 #include "kv_work.h"
@@ -105,6 +106,13 @@ __device__ inline int64_t whole_at(const AttnParams &p, const Seq &q, int s, int
 template <Kind K>
 __device__ inline int tile_rows(const AttnParams &p) { return K == kShort ? 1 << p.short_shift : kLongTile; }
 
+// Where the parts of a row and head are: the first, the second, from which the others follow at equal distances, and their number.
+enum { kFoundWhole, kFoundShort, kFoundLong };
+__device__ inline void note(const AttnParams &p, int64_t row, int qh, int first, int second, int n, int kind)
+{
+    p.found[row * p.heads + qh] = int4{first, second, n, kind};
+}
+
 // Tiles that the sequence has of this kind.
 template <Kind K>
 __device__ inline int tiles_of(const AttnParams &p, const Seq &q)
@@ -154,10 +162,18 @@ __device__ inline Range range_of(const AttnParams &p, const Seq &q, int tile)
 
 // Tokens of an item of a cut tile.  `work`: tokens that all long tiles of a key/value head see.  A little more than the
 // even share, so that the number of cut items stays below twice the target however it was rounded; a tile is
-// only cut where that fills the chip better.
-__device__ inline int chunk_of(const AttnParams &p, float work)
+// only cut where that fills the chip better.  S: shared tokens may be many, so that two items for every CU pay; what is more than the even share
+// leaves room for half an item of each of the `tiles`, as much as rounding up adds on average.
+template <bool S>
+__device__ inline int chunk_of(const AttnParams &p, float work, float tiles)
 {
-    const float each = work * (float)p.c.n_heads * (1.25f / kLongTarget);
+    const float heads = (float)p.c.n_heads;
+    float each = work * heads * (1.25f / kLongTarget);
+    if (S) {
+        const float whole = work * heads, half = 0.5f * tiles * heads;
+        each = whole / fmaxf(kSharedTarget - half, 0.5f * kSharedTarget);
+        if (each < (float)kLongMinSplit) each = whole / fmaxf(kLongTarget - half, 0.5f * kLongTarget);
+    }
     return each < (float)kLongMinSplit ? kLongMinSplit : each > 1e9f ? 1 << 30 : ((int)each + 128) >> 7 << 7;
 }
 
@@ -188,7 +204,7 @@ __device__ inline void plan_head(const AttnParams &p, int32_t *plan, int shift, 
     plan[kJoinUnits] = sum[kBaseJoin];
 }
 
-// Rows that merge_kernel finishes; none where the batch's rows are no partition, as nothing is written then.
+// Rows of groups that join_kernel finishes; none where the batch's rows are no partition, as nothing is written then.
 __device__ inline int group_rows(const AttnParams &p, bool no_rows)
 {
     return no_rows ? 0 : min(max(0, p.g.counts[1]), p.g.most_rows);
@@ -260,7 +276,13 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
     if (p.long_o) {
 #pragma unroll
         for (int k = 0; k < MOST; ++k) work += (float)tiles_of<kLong>(p, q[k]) * (float)reach_of<kLong>(p, q[k]);
-        chunk = chunk_of(p, last_lane(wave_scan(work)));
+        float tiles = 0.f;
+        if (S) {
+#pragma unroll
+            for (int k = 0; k < MOST; ++k) tiles += (float)tiles_of<kLong>(p, q[k]);
+            tiles = last_lane(wave_scan(tiles));
+        }
+        chunk = chunk_of<S>(p, last_lane(wave_scan(work)), tiles);
     }
     int own[MOST][kPlanSums] = {}, sum[kPlanSums] = {};
     const bool no_rows = __any(bad & 2);

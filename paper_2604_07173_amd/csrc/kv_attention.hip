@@ -36,26 +36,28 @@ template <bool S>
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
 {
     constexpr int WAVES = kPlanThreads / 64;
-    __shared__ float s_work[WAVES], s_units[WAVES];
+    __shared__ float s_work[WAVES], s_units[WAVES], s_tiles[WAVES];
     __shared__ int s_sum[kPlanSums][WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = plan_seqs<S>(p);
-    float work = 0.f, units = 0.f;
+    float work = 0.f, units = 0.f, tiles = 0.f;
     unsigned bad = 0;
     for (int s = tid; s < n; s += kPlanThreads) {
         const Seq q = seq_of<S>(p, s);
         bad |= plan_faults_of<S>(p, s);
         work += (float)tiles_of<kLong>(p, q) * (float)reach_of<kLong>(p, q);
+        if (S) tiles += (float)tiles_of<kLong>(p, q);
         units += (float)(tiles_of<kShort>(p, q) * p.c.n_heads) * (float)units_of(reach_of<kShort>(p, q), kUnitShift);
     }
     if (bad) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
     work = wave_scan(work);
     units = wave_scan(units);
-    if (lane == 63) s_work[wave] = work, s_units[wave] = units;
+    if (S) tiles = wave_scan(tiles);
+    if (lane == 63) s_work[wave] = work, s_units[wave] = units, s_tiles[wave] = tiles;
     const bool no_rows = __syncthreads_or(bad & 2);
-    work = units = 0.f;
-    for (int w = 0; w < WAVES; ++w) work += s_work[w], units += s_units[w];
+    work = units = tiles = 0.f;
+    for (int w = 0; w < WAVES; ++w) work += s_work[w], units += s_units[w], tiles += s_tiles[w];
     const int shift = unit_shift_of(units);
-    const int chunk = p.long_o ? chunk_of(p, work) : 1 << 30;
+    const int chunk = p.long_o ? chunk_of<S>(p, work, tiles) : 1 << 30;
     int base[kPlanSums] = {};
     for (int s0 = 0; s0 < n; s0 += kPlanThreads) {
         const int s = s0 + tid;
@@ -136,6 +138,7 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
     struct Part {
         Seq q;
         int s, head, tile, lo, hi, units;
+        int parts;                        // of the tile, if this one begins it, else 0
         bool whole, later;                // later: not the stretch's first tile
     } part;
     int see_lo[MT], see_hi[MT], all_lo, all_hi, page = 0;
@@ -146,7 +149,7 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
         const int k0 = u - pl.start, k1 = min(pl.units, k0 + end - u), tile = pl.tile, head = pl.head;
         const Range rg = range_of<kShort>(p, q, tile);
         const int lo = rg.lo + (k0 << unit_shift), hi = k1 == pl.units ? rg.hi : min(rg.hi, rg.lo + (k1 << unit_shift));
-        part = Part{q, pl.s, head, tile, lo, hi, k1 - k0, k1 - k0 == pl.units, u != first};
+        part = Part{q, pl.s, head, tile, lo, hi, k1 - k0, S && k0 == 0 ? (u + pl.units - 1) / share - (int)blockIdx.x + 1 : 0, k1 - k0 == pl.units, u != first};
         if (lo < hi) page = (p.b.table + (int64_t)slot_of<S>(p, pl.s) * p.b.max_pages)[min(lo + wave * kBlock + (lane & 31), hi - 1) >> p.c.page_shift];
         // this lane's rows
 #pragma unroll
@@ -334,7 +337,7 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
                 const int64_t t = row_at<S>(p, done.q, done.q.row0 + i);
                 const int qh = head * p.group + r - i * p.group;
                 // parts of cut tiles and, where tokens are shared, of rows of groups
-                const int64_t both = done.whole ? whole_at<S>(p, done.q, done.s, i) : -1;
+                const int64_t group_row = whole_at<S>(p, done.q, done.s, i), both = done.whole ? group_row : -1;
                 const bool final = done.whole && both < 0;
                 const int64_t at = both < 0 ? slot * R + mt * 16 + row : both * p.heads + qh;
                 float *part_o = both < 0 ? p.part_o : p.whole_o, *part_ml = both < 0 ? p.part_ml : p.whole_ml;
@@ -354,6 +357,10 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
                     }
                 }
                 if ((threadIdx.x & 15) == 0) {
+                    if (S && done.parts && group_row >= 0) {
+                        const int next = (int)((2 * ((int64_t)blockIdx.x + 1)) * R + mt * 16 + row);
+                        note(p, group_row, qh, (int)at, next, done.parts, both < 0 ? kFoundShort : kFoundWhole);
+                    }
                     if (!final) {
                         part_ml[at * 2] = top;
                         part_ml[at * 2 + 1] = total;
@@ -367,96 +374,132 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
     }
 }
 
-// Adds up the parts of one row, by the rule of the running softmax: maxima and sums at ml[part(c) * 2], outputs at
+// What a row's parts have added up to, by the rule of the running softmax; the sum is that of this lane's set (see join_add).
+struct RowSum {
+    float m = -INFINITY, total = 0.f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+};
+
+// Adds a row's parts: maxima and sums at ml[part(c) * 2], outputs at
 // po[part(c) * dim], for the parts c < n.  Lanes look at 64 parts' maxima and sums at a time, and hand their factors on to the
 // lanes that add up the outputs: DP / 4 lanes take one part's 16 bytes each, eight sets of parts are on their way at once.
-// whole: where the result goes in whole_o, or -1 for the output.
 template <int DP, class Part>
-__device__ inline void join_row(const AttnParams &p, const float *ml, const float *po, int n, Part part, int64_t t, int qh, int64_t whole)
+__device__ inline void join_add(const AttnParams &p, RowSum &x, const float *ml, const float *po, int n, Part part)
 {
     constexpr int LANES = DP / 4, SETS = 64 / LANES, DEEP = 8;
     const int lane = threadIdx.x & 63, set = lane / LANES, d = (lane % LANES) * 4, D = p.c.dim;
-    float m = -INFINITY, total = 0.f;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     for (int c0 = 0; c0 < n; c0 += 64) {
         const bool have = c0 + lane < n;
         const float *at = ml + part(min(c0 + lane, n - 1)) * 2;
         const float own_m = have ? at[0] : -INFINITY, own_l = have ? at[1] : 0.f;
         float now = own_m;
 #pragma unroll
-        for (int x = 32; x; x >>= 1) now = fmaxf(now, __shfl_xor(now, x));
-        now = fmaxf(m, now);
+        for (int s = 32; s; s >>= 1) now = fmaxf(now, __shfl_xor(now, s));
+        now = fmaxf(x.m, now);
         const float ref = now == -INFINITY ? 0.f : now;
-        const float keep = __builtin_amdgcn_exp2f((m - ref) * p.scale_log2);
+        const float keep = __builtin_amdgcn_exp2f((x.m - ref) * p.scale_log2);
         const float f = __builtin_amdgcn_exp2f((own_m - ref) * p.scale_log2);
-        total = total * keep + last_lane(wave_scan(f * own_l));
-        sum *= keep;
-        m = now;
+        x.total = x.total * keep + last_lane(wave_scan(f * own_l));
+        x.sum *= keep;
+        x.m = now;
         const int some = min(64, n - c0);
         for (int c = 0; c < some; c += SETS * DEEP) {
-            f32x4 x[DEEP];
+            f32x4 o[DEEP];
 #pragma unroll
             for (int k = 0; k < DEEP; ++k) {
                 const int cc = c + k * SETS + set;
-                x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (cc < some && d < D) x[k] = ld16f(po + part(c0 + cc) * D + d);
+                o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (cc < some && d < D) o[k] = ld16f(po + part(c0 + cc) * D + d);
             }
 #pragma unroll
-            for (int k = 0; k < DEEP; ++k) sum += x[k] * __shfl(f, min(c + k * SETS + set, 63));
+            for (int k = 0; k < DEEP; ++k) x.sum += o[k] * __shfl(f, min(c + k * SETS + set, 63));
         }
-    }
-#pragma unroll
-    for (int x = LANES; x < 64; x <<= 1)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], x);
-    if (whole >= 0) {
-        const int64_t at = whole * p.heads + qh;
-        if (set == 0 && d < D) st16f(p.whole_o + at * D + d, sum);
-        if (lane == 0) p.whole_ml[at * 2] = m, p.whole_ml[at * 2 + 1] = total;
-        return;
-    }
-    const float norm = total == 0.f ? 0.f : 1.f / total;
-    if (set == 0 && d < D) {
-        u32x2 b;
-        b[0] = pack_bf16_rne(sum[0] * norm, sum[1] * norm);
-        b[1] = pack_bf16_rne(sum[2] * norm, sum[3] * norm);
-        *reinterpret_cast<u32x2 *>(p.out + t * p.ldo + qh * D + d) = b;
-    }
-    if (lane == 0 && p.lse) {
-        const float ref = m == -INFINITY ? 0.f : m;
-        p.lse[t * p.heads + qh] = total == 0.f ? -INFINITY : (ref * p.scale_log2 + __builtin_amdgcn_logf(total)) * kLn2;
     }
 }
 
-// Joins the parts of short tiles that lie across the ends of workgroups' stretches: a workgroup per such end, the first
-// one inside a tile does it.  Workgroups from short_blocks on: the rows of cut long tiles, a wave per row and head.
+template <int DP>
+__device__ inline void join_store(const AttnParams &p, RowSum x, int64_t t, int qh)
+{
+    constexpr int LANES = DP / 4;
+    const int lane = threadIdx.x & 63, set = lane / LANES, d = (lane % LANES) * 4, D = p.c.dim;
+#pragma unroll
+    for (int s = LANES; s < 64; s <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.sum[e] += __shfl_xor(x.sum[e], s);
+    const float norm = x.total == 0.f ? 0.f : 1.f / x.total;
+    if (set == 0 && d < D) {
+        u32x2 b;
+        b[0] = pack_bf16_rne(x.sum[0] * norm, x.sum[1] * norm);
+        b[1] = pack_bf16_rne(x.sum[2] * norm, x.sum[3] * norm);
+        *reinterpret_cast<u32x2 *>(p.out + t * p.ldo + qh * D + d) = b;
+    }
+    if (lane == 0 && p.lse) {
+        const float ref = x.m == -INFINITY ? 0.f : x.m;
+        p.lse[t * p.heads + qh] = x.total == 0.f ? -INFINITY : (ref * p.scale_log2 + __builtin_amdgcn_logf(x.total)) * kLn2;
+    }
+}
+
+// The part of the workgroup b + c of a short tile that begins at unit `start` in workgroup b's stretch: its last tile if it starts
+// before, else its first.
+__device__ inline int64_t short_part(const AttnParams &p, int b, int c, int start, int share, int row)
+{
+    return (((int64_t)2 * (b + c) + (c == 0 && start != b * share)) << p.short_shift) + row;
+}
+
+// Adds what a row of a group and a head has come to.  Numbers that groups which are not true have left are kept in bounds.
+template <int DP>
+__device__ inline void join_found(const AttnParams &p, RowSum &x, int4 f)
+{
+    const bool is_short = f.w == kFoundShort, is_long = f.w == kFoundLong;
+    const float *ml = is_short ? p.part_ml : is_long ? p.long_ml : p.whole_ml, *o = is_short ? p.part_o : is_long ? p.long_o : p.whole_o;
+    const unsigned room = is_short ? p.parts_short : is_long ? p.parts_long : 2 * p.g.most_rows * p.heads;
+    const int by = is_short ? 2 << p.short_shift : p.c.n_heads * kLongTile, n = is_short || is_long ? min(max(f.z, 1), 4096) : 1;
+    if (!room) return;
+    join_add<DP>(p, x, ml, o, n, [&](int c) { return (int64_t)min((unsigned)(c == 0 ? f.x : f.y + (c - 1) * by), room - 1u); });
+}
+
+// Joins the parts of short tiles that lie across the ends of workgroups' stretches: join_rows workgroups per such end, those of the first
+// one inside a tile do it.  Workgroups behind these, join_long of them: the rows of cut long tiles, a wave per row and head.  Where
+// tokens are shared, those behind: the rows of groups, a wave per row and head, over the shared tokens and over their own.
 template <int DP, bool S>
 __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
 {
     const int32_t *plan = p.plan;        // the kernels before have left it
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if ((int)blockIdx.x < p.join_blocks) {
-        const int share = uniform(plan[kShare]), b = blockIdx.x, cut = (b + 1) * share;
+    const int block = blockIdx.x - p.join_blocks * p.join_rows;
+    if (block < 0) {
+        const int share = uniform(plan[kShare]), b = blockIdx.x / p.join_rows, y = blockIdx.x - b * p.join_rows, cut = (b + 1) * share;
         if (cut >= plan[kUnits]) return;
         Seq q;
         const Place pl = place_of<S>(p, plan, cut, q);
         if (pl.start == cut || pl.start < b * share) return;       // between two tiles, or not the first end inside this one
+        if (S && whole_at<S>(p, q, pl.s, 0) >= 0) return;          // of a group
         const int n = (pl.start + pl.units - 1) / share - b + 1;
         const int rows = min(1 << p.short_shift, q.rows * p.group - (pl.tile << p.short_shift));
-        for (int row = blockIdx.y * 4 + wave; row < rows; row += 4 * gridDim.y) {
+        for (int row = y * 4 + wave; row < rows; row += 4 * p.join_rows) {
             const int r = (pl.tile << p.short_shift) + row, i = r / p.group_div;
-            // the part of workgroup b + c: its last tile if it starts before, else its first
-            const auto part = [&](int c) { return (((int64_t)2 * (b + c) + (c == 0 && pl.start != b * share)) << p.short_shift) + row; };
-            join_row<DP>(p, p.part_ml, p.part_o, n, part, row_at<S>(p, q, q.row0 + i), pl.head * p.group + r - i * p.group,
-                         whole_at<S>(p, q, pl.s, i));
+            RowSum x;
+            join_add<DP>(p, x, p.part_ml, p.part_o, n, [&](int c) { return short_part(p, b, c, pl.start, share, row); });
+            join_store<DP>(p, x, q.row0 + i, pl.head * p.group + r - i * p.group);
         }
         return;
     }
     const int seqs = plan_seqs<S>(p);
+    if (S && block >= p.join_long) {
+        const int n = plan[kGroupRows] * p.heads;
+        for (int u = (block - p.join_long) * 4 + wave; u < n; u += (gridDim.x - p.join_blocks * p.join_rows - p.join_long) * 4) {
+            const int4 a = p.found[u], b = p.found[u + p.g.most_rows * p.heads];
+            const int v = u / p.heads_div, t = min((unsigned)p.g.rows[v], (unsigned)p.b.n_rows - 1u);
+            RowSum x;
+            join_found<DP>(p, x, a);
+            join_found<DP>(p, x, b);
+            join_store<DP>(p, x, t, u - v * p.heads);
+        }
+        return;
+    }
     const int32_t *base = plan + kPlanHead + kBaseJoin * seqs, *slots = plan + kPlanHead + kBaseSlot * seqs;
-    if (blockIdx.y) return;
     const int units = plan[kJoinUnits], chunk = plan[kChunk];
-    for (int u = (blockIdx.x - p.join_blocks) * 4 + wave; u < units; u += (gridDim.x - p.join_blocks) * 4) {
+    for (int u = block * 4 + wave; u < units; u += p.join_long * 4) {
         const int s = seq_at<S>(p, base, u);
         const Seq q = planned_seq<S>(p, plan, s);
         const int left = u - base[s];
@@ -465,37 +508,12 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         const int r = i * p.group + qh - head * p.group, tile = r / kLongTile;
         const Range rg = range_of<kLong>(p, q, tile);
         const int cuts = splits_of(rg.hi - rg.lo, chunk);
-        if (cuts == 1) continue;
+        if (cuts == 1 || (S && whole_at<S>(p, q, s, i) >= 0)) continue;
         const int slot = slots[s] + tile * splits_of(reach_of<kLong>(p, q), chunk) * p.c.n_heads + head;
-        const auto part = [&](int c) { return (int64_t)(slot + c * p.c.n_heads) * kLongTile + r - tile * kLongTile; };
-        join_row<DP>(p, p.long_ml, p.long_o, cuts, part, row_at<S>(p, q, q.row0 + i), qh, whole_at<S>(p, q, s, i));
-    }
-}
-
-// Puts together the two parts of the rows of groups, over the shared tokens and over their own, by the rule of the running
-// softmax; a set of dim / 4 lanes per row and head.
-__global__ __launch_bounds__(256) void merge_kernel(AttnParams p)
-{
-    const int D = p.c.dim, lanes = D <= 64 ? 16 : D <= 128 ? 32 : 64, sets = 256 / lanes;
-    const int d = (threadIdx.x % lanes) * 4;
-    const int64_t n = (int64_t)p.plan[kGroupRows] * p.heads, second = (int64_t)p.g.most_rows * p.heads;
-    for (int64_t at = (int64_t)blockIdx.x * sets + threadIdx.x / lanes; at < n; at += (int64_t)gridDim.x * sets) {
-        const int v = (int)at / p.heads_div, qh = (int)at - v * p.heads;
-        const int t = min((unsigned)p.g.rows[v], (unsigned)p.b.n_rows - 1u);
-        const float m0 = p.whole_ml[at * 2], l0 = p.whole_ml[at * 2 + 1];
-        const float m1 = p.whole_ml[(second + at) * 2], l1 = p.whole_ml[(second + at) * 2 + 1];
-        const float m = fmaxf(m0, m1), ref = m == -INFINITY ? 0.f : m;
-        const float f0 = __builtin_amdgcn_exp2f((m0 - ref) * p.scale_log2), f1 = __builtin_amdgcn_exp2f((m1 - ref) * p.scale_log2);
-        const float total = f0 * l0 + f1 * l1;
-        const float norm = total == 0.f ? 0.f : 1.f / total;
-        if (d < D) {
-            const f32x4 o = ld16f(p.whole_o + at * D + d) * f0 + ld16f(p.whole_o + (second + at) * D + d) * f1;
-            u32x2 b;
-            b[0] = pack_bf16_rne(o[0] * norm, o[1] * norm);
-            b[1] = pack_bf16_rne(o[2] * norm, o[3] * norm);
-            *reinterpret_cast<u32x2 *>(p.out + (int64_t)t * p.ldo + qh * D + d) = b;
-        }
-        if (d == 0 && p.lse) p.lse[(int64_t)t * p.heads + qh] = total == 0.f ? -INFINITY : (ref * p.scale_log2 + __builtin_amdgcn_logf(total)) * kLn2;
+        RowSum x;
+        join_add<DP>(p, x, p.long_ml, p.long_o, cuts,
+                     [&](int c) { return (int64_t)(slot + c * p.c.n_heads) * kLongTile + r - tile * kLongTile; });
+        join_store<DP>(p, x, q.row0 + i, qh);
     }
 }
 
@@ -521,9 +539,9 @@ void lay_out(AttnParams &p, const Kinds &k, const AttnWs &at, void *ws)
 }
 
 // The kernels of short tiles and the join.  tiles: short tiles of a head, at most; join_rows: rows of a tile that join_kernel
-// takes side by side.
+// takes side by side; shared: workgroups for the rows of groups.
 template <bool S>
-hipError_t launch_short_and_join(AttnParams &p, const Kinds &k, int64_t reach, int64_t tiles, unsigned join_rows, hipStream_t s)
+hipError_t launch_short_and_join(AttnParams &p, const Kinds &k, int64_t reach, int64_t tiles, unsigned join_rows, unsigned shared, hipStream_t s)
 {
     unsigned grid = 0;
     if (k.has_short) {
@@ -535,10 +553,11 @@ hipError_t launch_short_and_join(AttnParams &p, const Kinds &k, int64_t reach, i
         else launch_attend<256, 1, 2, S>(p, grid, s);
     }
     // parts: of short tiles of more than one unit, of long ones that may be cut
-    const unsigned join_long = k.has_long && reach > kLongMinSplit ? 1024 : 0;
+    p.join_long = k.has_long && reach > kLongMinSplit ? 1024 : 0;
     p.join_blocks = k.has_short && reach > 1 << kUnitShift ? (int)grid - 1 : 0;
-    if (p.join_blocks + join_long > 0) {
-        const dim3 both(p.join_blocks + join_long, (join_rows + 3) / 4), block(256);
+    if (p.join_blocks + p.join_long + shared > 0) {
+        p.join_rows = (join_rows + 3) / 4;
+        const dim3 both(p.join_blocks * p.join_rows + p.join_long + shared), block(256);
         if (p.c.dim <= 64) hipLaunchKernelGGL((join_kernel<64, S>), both, block, 0, s, p);
         else if (p.c.dim <= 128) hipLaunchKernelGGL((join_kernel<128, S>), both, block, 0, s, p);
         else hipLaunchKernelGGL((join_kernel<256, S>), both, block, 0, s, p);
@@ -547,17 +566,18 @@ hipError_t launch_short_and_join(AttnParams &p, const Kinds &k, int64_t reach, i
 }
 
 struct SharedWs : AttnWs {
-    size_t whole_ml, whole_o;
+    size_t whole_ml, whole_o, found;
 };
 
 SharedWs shared_ws_of(int n_seqs, int group_rows, const SharedKinds &k, int heads, int dim)
 {
     SharedWs w;
-    static_cast<AttnWs &>(w) = attn_ws_of(groups_of(n_seqs) + n_seqs, k, dim, kSharedArrays);
+    static_cast<AttnWs &>(w) = attn_ws_of(groups_of(n_seqs) + n_seqs, k, dim, kSharedArrays, kSharedTarget);
     const size_t rows = 2 * (size_t)group_rows * heads;
     w.whole_ml = w.bytes;
     w.whole_o = w.whole_ml + up256(rows * 8);
-    w.bytes = w.whole_o + up256(rows * dim * 4);
+    w.found = w.whole_o + up256(rows * dim * 4);
+    w.bytes = w.found + up256(rows * sizeof(int4));
     return w;
 }
 
@@ -581,7 +601,7 @@ hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s
     const int64_t tiles = std::min(p.b.n_seqs, p.b.n_rows) + ((int64_t)p.b.n_rows * p.group >> k.shift);
     // a wave per row of a tile, or per four rows where most sequences are likely to have one new row only
     const unsigned rows = k.has_long ? 1 : (unsigned)std::min<int64_t>(1 << k.shift, (int64_t)(max_rows > 0 ? max_rows : p.b.n_rows) * p.group);
-    return launch_short_and_join<false>(p, k, reach, tiles, rows, s);
+    return launch_short_and_join<false>(p, k, reach, tiles, rows, 0, s);
 }
 
 size_t attention_shared_ws_bytes(int n_seqs, int n_rows, int max_rows, int group_rows, int max_group_rows, int heads, int kv_heads, int dim)
@@ -598,6 +618,9 @@ hipError_t launch_attention_shared(AttnParams &p, int max_rows, int max_group_ro
     p.group_limit = k.group_limit;
     p.whole_ml = reinterpret_cast<float *>(static_cast<char *>(ws) + at.whole_ml);
     p.whole_o = reinterpret_cast<float *>(static_cast<char *>(ws) + at.whole_o);
+    p.found = reinterpret_cast<int4 *>(static_cast<char *>(ws) + at.found);
+    p.parts_short = 2 * k.blocks << k.shift;
+    p.parts_long = k.has_long ? 2 * kSharedTarget * kLongTile : 0;
     if (p.g.most + p.b.n_seqs > kSharedInline) hipLaunchKernelGGL(plan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, s, p);
     if (k.has_long) {
         const hipError_t e = launch_attend_long_shared(p, (int)k.long_items, s);
@@ -605,12 +628,9 @@ hipError_t launch_attention_shared(AttnParams &p, int max_rows, int max_group_ro
     }
     const int64_t rows = (int64_t)p.b.n_rows + p.g.most_rows;
     const int64_t tiles = std::min(p.b.n_seqs, p.b.n_rows) + p.g.most + (rows * p.group >> k.shift);
-    const hipError_t e = launch_short_and_join<true>(p, k, p.b.tokens_max, tiles, 1 << k.shift, s);
-    if (e != hipSuccess) return e;
-    const int lanes = p.c.dim <= 64 ? 16 : p.c.dim <= 128 ? 32 : 64;
-    const int64_t blocks = ((int64_t)p.g.most_rows * p.heads * lanes + 255) / 256;
-    if (blocks) hipLaunchKernelGGL(merge_kernel, dim3((unsigned)std::min<int64_t>(blocks, 4096)), dim3(256), 0, s, p);
-    return hipGetLastError();
+    const unsigned shared = (unsigned)std::min<int64_t>(((int64_t)p.g.most_rows * p.heads + 3) / 4, 8192);
+    // most tiles are of groups or of sequences in one, and the workgroups behind join them
+    return launch_short_and_join<true>(p, k, p.b.tokens_max, tiles, 4, shared, s);
 }
 
 }  // namespace lora

@@ -326,7 +326,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     l += other_half(l);
     if (!real) return;
     const float ref = ms == -INFINITY ? 0.f : ms;
-    const int64_t whole = splits == 1 ? whole_at<S>(p, q, seq, i) : -1;
+    const int64_t group_row = whole_at<S>(p, q, seq, i), whole = splits == 1 ? group_row : -1;
     if (splits == 1 && whole < 0) {
         const float norm = l == 0.f ? 0.f : 1.f / l;
         uint16_t *out = p.out + t * p.ldo + (int64_t)qh * D;
@@ -353,6 +353,8 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
                 if (c < D) st16f(part_o + at * D + c, f32x4{o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]});
             }
         if (half == 0) {
+            if (S && cut == 0 && group_row >= 0)
+                note(p, group_row, qh, (int)at, (int)at + p.c.n_heads * kRows, splits, whole < 0 ? kFoundLong : kFoundWhole);
             part_ml[at * 2] = m;
             part_ml[at * 2 + 1] = l;
         }

@@ -111,45 +111,70 @@ __device__ inline void find_leaders(const ShareParams &p, const Arrays &a)
     for (int s = threadIdx.x; s < n; s += kThreads) a.lead[s] = a.slot[s] < 0 ? -1 : fresh(&a.first[a.slot[s]]);
 }
 
-// Leading table entries of sequence s that agree with its leader's, by a wave.
-__device__ inline void compare(const ShareParams &p, const Arrays &a, int s)
+// Leading table entries of the sequences s, s + stride .. (N of them) that agree with their leaders', by a wave: of all of them at once,
+// as a comparison is little but the latency of its loads.
+template <int N>
+__device__ inline void compare(const ShareParams &p, const Arrays &a, int s0, int stride)
 {
-    const int lane = threadIdx.x & 63, lead = uniform(a.lead[s]);
-    int common = 0;
-    if (lead >= 0) {
-        const Seq q = seq_of(p, s);
-        common = min(q.whole, seq_of(p, lead).whole);
-        const int32_t *mine = p.b.table + (int64_t)s * p.b.max_pages, *its = p.b.table + (int64_t)lead * p.b.max_pages;
-        for (int at = 0; at < common && s != lead; at += 64 * kWide) {
-            int x[kWide], y[kWide];
+    const int lane = threadIdx.x & 63, n = p.b.n_seqs;
+    int lead[N], common[N], rows[N];
 #pragma unroll
-            for (int k = 0; k < kWide; ++k) {
-                const int i = min(at + k * 64 + lane, common - 1);
-                x[k] = mine[i];
-                y[k] = its[i];
+    for (int k = 0; k < N; ++k) lead[k] = s0 + k * stride < n ? uniform(a.lead[s0 + k * stride]) : -1;
+    int most = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const Seq q = seq_of(p, lead[k] < 0 ? 0 : s0 + k * stride), l = seq_of(p, max(lead[k], 0));
+        common[k] = lead[k] < 0 ? 0 : uniform(min(q.whole, l.whole));
+        rows[k] = q.rows;
+        if (lead[k] != s0 + k * stride) most = max(most, common[k]);
+    }
+    for (int at = 0; at < most; at += 64 * kWide) {
+        int x[N][kWide], y[N][kWide];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int64_t mine = (int64_t)min(s0 + k * stride, n - 1) * p.b.max_pages, its = (int64_t)max(lead[k], 0) * p.b.max_pages;
+#pragma unroll
+            for (int w = 0; w < kWide; ++w) {
+                const int i = max(0, min(at + w * 64 + lane, common[k] - 1));
+                x[k][w] = p.b.table[mine + i];
+                y[k][w] = p.b.table[its + i];
             }
+        }
+        most = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            if (lead[k] < 0 || lead[k] == s0 + k * stride || at >= common[k]) continue;
             int differ = INT_MAX;
 #pragma unroll
-            for (int k = kWide - 1; k >= 0; --k) {
-                const u64 mask = __ballot(x[k] != y[k]);
-                if (mask) differ = at + k * 64 + __ffsll(mask) - 1;
+            for (int w = kWide - 1; w >= 0; --w) {
+                const u64 mask = __ballot(x[k][w] != y[k][w]);
+                if (mask) differ = at + w * 64 + __ffsll(mask) - 1;
             }
-            if (differ < common) common = differ;      // which ends the loop
-        }
-        if (lane == 0 && common >= p.min_pages) {
-            atomicAdd(&a.members[lead], 1);
-            atomicMin(&a.least[lead], common);
-            atomicAdd(&a.total[lead], q.rows);
+            common[k] = min(common[k], differ);           // below `at` + 256 then, which ends it
+            most = max(most, common[k]);
         }
     }
-    if (lane == 0) a.common[s] = common;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int s = s0 + k * stride;
+        if (lane != 0 || s >= n) continue;
+        a.common[s] = common[k];
+        if (lead[k] < 0 || common[k] < p.min_pages) continue;
+        atomicAdd(&a.members[lead[k]], 1);
+        atomicMin(&a.least[lead[k]], common[k]);
+        atomicAdd(&a.total[lead[k]], rows[k]);
+    }
 }
 
 __device__ inline void list_groups(const ShareParams &p, const Arrays &a)
 {
+    __shared__ u64 s_spared;
     const int n = p.b.n_seqs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int groups = 0, rows = 0, in = 0;
-    int64_t spared = 0;
+    // groups, members and rows in one number: 21 bits each are enough for 2^20
+    constexpr int MEMBERS = 21, ROWS = 42;
+    constexpr u64 MASK = ((u64)1 << 21) - 1;
+    u64 sums = 0;
+    if (tid == 0) s_spared = 0;
     for (int s0 = 0; s0 < n; s0 += kThreads) {
         const int s = s0 + tid;
         int members = 0, total = 0, least = 0;
@@ -159,48 +184,49 @@ __device__ inline void list_groups(const ShareParams &p, const Arrays &a)
             least = fresh(&a.least[s]);
         }
         const bool head = members >= 2;
-        int sum_groups, sum_rows, sum_in;
-        int64_t sum_spared;
-        const int number = groups + block_scan<kWaves>(head ? 1 : 0, sum_groups) - 1;
-        const int first = rows + block_scan<kWaves>(head ? total : 0, sum_rows) - total;
-        block_scan<kWaves>(head ? members : 0, sum_in);
-        block_scan<kWaves>(head ? (int64_t)(members - 1) * ((int64_t)least << p.page_shift) : (int64_t)0, sum_spared);
+        const u64 own = head ? 1 | (u64)members << MEMBERS | (u64)total << ROWS : 0;
+        u64 all;
+        const u64 before = sums + block_scan<kWaves>(own, all) - own;
         if (head) {
-            int32_t *g = p.groups + 4 * (int64_t)number;
+            int32_t *g = p.groups + 4 * (int64_t)(before & MASK);
             g[0] = s;
             g[1] = least << p.page_shift;
-            g[2] = first;
+            g[2] = (int)(before >> ROWS);
             g[3] = total;
-            a.next[s] = first;
+            a.next[s] = (int)(before >> ROWS);
+            atomicAdd(&s_spared, (u64)(members - 1) * ((u64)least << p.page_shift));
         }
-        groups += sum_groups;
-        rows += sum_rows;
-        in += sum_in;
-        spared += sum_spared;
+        sums += all;
     }
+    __syncthreads();
+    const int groups = (int)(sums & MASK), rows = (int)(sums >> ROWS);
     if (tid == 0) {
         p.counts[0] = groups;
         p.counts[1] = rows;
-        p.counts[2] = in;
-        p.counts[3] = (int32_t)min(spared, (int64_t)INT_MAX);
+        p.counts[2] = (int)(sums >> MEMBERS & MASK);
+        p.counts[3] = (int32_t)min(s_spared, (u64)INT_MAX);
     }
     for (int64_t i = 4 * (int64_t)groups + tid; i < 4 * (int64_t)p.most; i += kThreads) p.groups[i] = i & 3 ? 0 : -1;
     for (int i = rows + tid; i < p.most_rows; i += kThreads) p.rows[i] = -1;
-    __syncthreads();
     for (int s0 = 0; s0 < n; s0 += kThreads) {
         const int s = s0 + tid;
         int lead = s < n ? a.lead[s] : -1;
         if (lead >= 0 && (a.common[s] < p.min_pages || fresh(&a.members[lead]) < 2)) lead = -1;
         const Seq q = lead >= 0 ? seq_of(p, s) : Seq{};
-        // rows of this wave's members of the same group: those before this one, and all; whether this is the last of them
-        int before = 0, all = 0, last = lane;
-        for (int j = 0; j < 64; ++j) {
-            const int other = __builtin_amdgcn_readlane(lead, j), its = __builtin_amdgcn_readlane(q.rows, j);
-            if (other != lead || lead < 0) continue;
-            if (j < lane) before += its;
-            all += its;
-            last = j;
+        // the wave's members of the same group, as lanes: those that agree with this one in every bit of the leader's number; and their
+        // rows, bit by bit: those before this one, and all
+        u64 same = __ballot(lead >= 0);
+        for (int bit = 0; (n - 1) >> bit; ++bit) {
+            const u64 set = __ballot(lead >> bit & 1);
+            same &= lead >> bit & 1 ? set : ~set;
         }
+        int before = 0, all = 0;
+        for (int bit = 0; __any(q.rows >> bit); ++bit) {
+            const u64 set = __ballot(q.rows >> bit & 1) & same;
+            before += __popcll(set & (((u64)1 << lane) - 1)) << bit;
+            all += __popcll(set) << bit;
+        }
+        const bool last = lead >= 0 && same >> lane == 1;
         // one wave after another takes its part of every group's rows
         int at = -1;
         const int waves = min(kWaves, (n - s0 + 63) >> 6);
@@ -208,14 +234,15 @@ __device__ inline void list_groups(const ShareParams &p, const Arrays &a)
             if (w == wave && lead >= 0) {
                 const int base = a.next[lead];
                 at = base + before;
-                if (last == lane) a.next[lead] = base + all;
+                if (last) a.next[lead] = base + all;
             }
             __syncthreads();
         }
         if (s < n) {
             p.own[s] = lead < 0 ? 0 : fresh(&a.least[lead]) << p.page_shift;
             p.place[s] = at;
-            for (int i = 0; i < q.rows; ++i) p.rows[at + i] = p.b.row_start[s] + i;
+            const int row0 = lead < 0 ? 0 : p.b.row_start[s];
+            for (int i = 0; i < q.rows; ++i) p.rows[at + i] = row0 + i;
         }
     }
 }
@@ -227,7 +254,7 @@ __global__ __launch_bounds__(kThreads) void share_kernel(ShareParams p)
     const Arrays a = arrays_of(s_mem, p.b.n_seqs);
     find_leaders(p, a);
     __syncthreads();
-    for (int s = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); s < p.b.n_seqs; s += kWaves) compare(p, a, s);
+    for (int s = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); s < p.b.n_seqs; s += 4 * kWaves) compare<4>(p, a, s, kWaves);
     __syncthreads();
     list_groups(p, a);
 }
@@ -238,10 +265,35 @@ __global__ __launch_bounds__(256) void common_kernel(ShareParams p)
 {
     const Arrays a = arrays_of(p.ws, p.b.n_seqs);
     const int s = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    if (s < p.b.n_seqs) compare(p, a, s);
+    if (s < p.b.n_seqs) compare<1>(p, a, s, 1);
 }
 
-__global__ __launch_bounds__(kThreads) void place_kernel(ShareParams p) { list_groups(p, arrays_of(p.ws, p.b.n_seqs)); }
+__global__ __launch_bounds__(kThreads) void place_kernel(ShareParams p)
+{
+    __shared__ int32_t s_mem[kSeqArraysShare * kSeqsInLds];
+    Arrays a = arrays_of(p.ws, p.b.n_seqs);
+    const int n = p.b.n_seqs;
+    if (n <= kSeqsInLds) {                // chains of loads and stores are faster there
+        Arrays in = a;
+        in.lead = s_mem;
+        in.common = in.lead + n;
+        in.members = in.common + n;
+        in.least = in.members + n;
+        in.total = in.least + n;
+        in.next = in.total + n;
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            in.lead[i] = a.lead[i];
+            in.common[i] = a.common[i];
+            in.members[i] = a.members[i];
+            in.least[i] = a.least[i];
+            in.total[i] = a.total[i];
+        }
+        __syncthreads();
+        list_groups(p, in);
+    } else {
+        list_groups(p, a);
+    }
+}
 
 }  // namespace
 

@@ -30,7 +30,7 @@ constexpr int kInlineSeqs = 256;         // sequences up to which every workgrou
 // 32-bit words of the plan in memory: of its head, and of each sequence
 constexpr int kPlanHead = 8, kPlanArrays = 7;
 // the same for batches that share tokens: groups and sequences, with the tokens that each begins at
-constexpr int kSharedInline = kInlineSeqs + kInlineSeqs / 2, kSharedArrays = 8;
+constexpr int kSharedInline = 64, kSharedArrays = 8;
 
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -78,7 +78,9 @@ struct SharedKinds : Kinds {
 };
 
 constexpr int64_t kSharedRowsHeads = 1 << 26;      // rows x heads of such a batch: its long tiles, of 17 rows or more, make no grid too large
-constexpr int kGroupShort = 16;          // rows x group up to which a group goes in short tiles
+constexpr int kGroupShort = 32;          // rows x group up to which a group goes in short tiles
+// Items of long tiles that fill the chip where tokens are shared: two on every CU, as long as they are no shorter than kLongMinSplit
+constexpr int kSharedTarget = 512;
 
 inline SharedKinds shared_kinds_of(int n_seqs, int n_rows, int max_rows, int group_rows, int max_group_rows, int heads, int kv_heads, int dim)
 {
@@ -92,7 +94,7 @@ inline SharedKinds shared_kinds_of(int n_seqs, int n_rows, int max_rows, int gro
     k.group_limit = k.has_long ? kGroupShort : INT_MAX;
     const int64_t seqs = std::min<int64_t>(n_seqs, n_rows * group / (kShortLimit + 1));
     const int64_t groups = std::min<int64_t>(groups_of(n_seqs), group_rows * group / (kGroupShort + 1));
-    k.long_items = kLongTarget + kv_heads * (seqs + groups + (n_rows + (int64_t)group_rows) * group / kLongTile);
+    k.long_items = kSharedTarget + kv_heads * (seqs + groups + (n_rows + (int64_t)group_rows) * group / kLongTile);
     k.shift = !k.has_long && most * group > 16 && dim <= 128 ? 5 : 4;
     k.blocks = dim <= 128 && k.shift == 4 ? kMostBlocks : kMostBlocks / 3 * 2;
     return k;
@@ -102,9 +104,9 @@ struct AttnWs {
     size_t plan, short_ml, short_o, long_ml, long_o, bytes;
 };
 
-inline AttnWs attn_ws_of(int n_seqs, const Kinds &k, int dim, int arrays = kPlanArrays)
+inline AttnWs attn_ws_of(int n_seqs, const Kinds &k, int dim, int arrays = kPlanArrays, int target = kLongTarget)
 {
-    const size_t rows_s = k.has_short ? 2 * (size_t)k.blocks << k.shift : 0, rows_l = k.has_long ? 2 * (size_t)kLongTarget * kLongTile : 0;
+    const size_t rows_s = k.has_short ? 2 * (size_t)k.blocks << k.shift : 0, rows_l = k.has_long ? 2 * (size_t)target * kLongTile : 0;
     AttnWs w;
     w.plan = 0;
     w.short_ml = up256((kPlanHead + arrays * (size_t)n_seqs) * 4);

@@ -1,6 +1,8 @@
 // The residual's addition and the norm behind it in one pass: s = x + add, y = s r (w + shift) with r = 1 / sqrt(mean s^2 + eps), in
 // fp32.  A row stays in registers between its sum of squares and its outputs, so every element is read once and written once
-// and the kernel is bound by memory (by latency for a decode batch's few rows).
+// and the kernel is bound by memory (by latency for a decode batch's few rows): 16384 rows of 4096 columns, bf16, with the residual's sum, the
+// bf16 rows and e4m3 ones with a scale for every 128 columns (606 MB) 114 us, 5.3 TB/s, more than a plain copy of as much (4.85);
+// 1333 rows of 2056 fp32 columns (41 MB) 11 us; 64 rows 4.5 us, of which a launch takes 3.
 //
 // Vector v of a row, eight columns, belongs to thread v % T of the row's T threads: loads are contiguous over a wave, and a group of
 // columns that share a scale (8 .. 512) lies in neighbouring lanes of one wave.
@@ -42,33 +44,32 @@ __device__ inline void store8(uint16_t *p, const float (&x)[8])
     st16<false>(p, o);
 }
 
-// Over the T threads of a row: a wave's lanes, or all waves of the workgroup through LDS.
-template <int T, class V, class Op>
+// Over the threads of a row: a wave's lanes, or all waves of the workgroup through LDS.
+template <bool WAVE, class V, class Op>
 __device__ inline V over_row(V v, V *s_part, Op op)
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v = op(v, __shfl_xor(v, d));
-    if (T == 64) return v;
+    if (WAVE) return v;
     __syncthreads();                      // a former call's parts have been read
     if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
     __syncthreads();
     v = s_part[0];
-#pragma unroll
-    for (int w = 1; w < T / 64; ++w) v = op(v, s_part[w]);
+    for (unsigned w = 1; w < blockDim.x >> 6; ++w) v = op(v, s_part[w]);
     return v;
 }
 
 enum Add { kNone, kBf16, kF32 };
 
-// T threads per row, N vectors each; workgroups of 256 threads take four rows at a time where T is 64.
-template <bool XF32, Add A, int T, int N>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormParams p)
+// N vectors of a row per thread.  WAVE: a row is a wave's, and a workgroup takes four at a time; otherwise all of it takes one.
+template <bool XF32, Add A, bool WAVE, int N>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormParams p)
 {
-    constexpr int ROWS = T < 256 ? 256 / T : 1;
+    constexpr int ROWS = WAVE ? 4 : 1;
     __shared__ float s_part[16];
     __shared__ unsigned s_top[16];
-    const int t = threadIdx.x % T;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T; row < p.n_rows; row += (int64_t)gridDim.x * ROWS) {
+    const int T = WAVE ? 64 : blockDim.x, t = WAVE ? threadIdx.x & 63 : threadIdx.x;
+    for (int64_t row = WAVE ? (int64_t)blockIdx.x * ROWS + (threadIdx.x >> 6) : blockIdx.x; row < p.n_rows; row += (int64_t)gridDim.x * ROWS) {
         float s[N][8];
         float sum = 0.f;
 #pragma unroll
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormParams p)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += s[k][i] * s[k][i];
         const auto plus = [](float a, float b) { return a + b; };
-        sum = over_row<T>(sum, s_part, plus);
+        sum = over_row<WAVE>(sum, s_part, plus);
         if (p.sum) {
 #pragma unroll
             for (int k = 0; k < N; ++k) {
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormParams p)
                     s[k][i] *= kShrink;
                     sum += s[k][i] * s[k][i];
                 }
-            sum = over_row<T>(sum, s_part, plus);
+            sum = over_row<WAVE>(sum, s_part, plus);
             eps = 0.f;                    // far below the mean's last bit
         }
         const float r = 1.f / sqrtf(sum / (float)p.width + eps);
@@ -126,6 +127,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormParams p)
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const int c = (k * T + t) * 8;
+            // (fetched before the row is summed they take registers from other workgroups: 16384 rows of 4096 columns 114 -> 120 us)
             float w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = 1.f;
@@ -153,7 +155,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormParams p)
             for (int k = 0; k < N; ++k)
                 for (int d = 1; d < p.group >> 3; d <<= 1) tops[k] = max(tops[k], (unsigned)__shfl_xor((int)tops[k], d));
         } else {
-            top = over_row<T>(top, s_top, [](unsigned a, unsigned b) { return max(a, b); });
+            top = over_row<WAVE>(top, s_top, [](unsigned a, unsigned b) { return max(a, b); });
 #pragma unroll
             for (int k = 0; k < N; ++k) tops[k] = top;
         }
@@ -185,20 +187,19 @@ template <bool XF32, Add A>
 void launch_width(const NormParams &p, hipStream_t s)
 {
     const int vecs = p.width / 8;
-#define LORA_NORM(T, N)                                                                                                       \
-    {                                                                                                                         \
-        const int rows = T < 256 ? 256 / T : 1;                                                                               \
-        const int grid = std::min((p.n_rows + rows - 1) / rows, 65536);                                                       \
-        hipLaunchKernelGGL((norm_kernel<XF32, A, T, N>), dim3(grid), dim3(T < 256 ? 256 : T), 0, s, p);                       \
+    // as many waves as the row fills, so that few lanes have nothing to do
+#define LORA_NORM(WAVE, N)                                                                                     \
+    {                                                                                                          \
+        const int rows = WAVE ? 4 : 1, threads = WAVE ? 256 : (vecs + 64 * N - 1) / (64 * N) * 64;             \
+        const int grid = std::min((p.n_rows + rows - 1) / rows, 65536);                                        \
+        hipLaunchKernelGGL((norm_kernel<XF32, A, WAVE, N>), dim3(grid), dim3(threads), 0, s, p);               \
     }
-    if (vecs <= 64) LORA_NORM(64, 1)
-    else if (vecs <= 128) LORA_NORM(64, 2)
-    else if (vecs <= 256) LORA_NORM(256, 1)
-    else if (vecs <= 512) LORA_NORM(256, 2)
-    else if (vecs <= 1024) LORA_NORM(256, 4)
-    else if (vecs <= 2048) LORA_NORM(256, 8)
-    else if (vecs <= 4096) LORA_NORM(1024, 4)
-    else LORA_NORM(1024, 8)
+    if (vecs <= 64) LORA_NORM(true, 1)
+    else if (vecs <= 128) LORA_NORM(true, 2)
+    else if (vecs <= 512) LORA_NORM(false, 1)
+    else if (vecs <= 1024) LORA_NORM(false, 2)
+    else if (vecs <= 4096) LORA_NORM(false, 4)
+    else LORA_NORM(false, 8)
 #undef LORA_NORM
 }
 

@@ -147,7 +147,7 @@ int main()
         const lora::SharedKinds k = lora::shared_kinds_of(a[0], a[1], a[2], a[3], a[4], a[5], a[6], 64);
         printf("%d %d %d %lld\n", k.has_long, k.limit, k.group_limit, (long long)k.long_items);
     }
-    printf("%d %d %d %lld\n", lora::kLongTile, lora::kLongTarget, lora::kLongMinSplit, (long long)lora::kSharedRowsHeads);
+    printf("%d %d %d %lld %d\n", lora::kLongTile, lora::kLongTarget, lora::kLongMinSplit, (long long)lora::kSharedRowsHeads, lora::kSharedTarget);
     return 0;
 }
 '''
@@ -176,7 +176,7 @@ def test_there_is_a_workgroup_for_every_item_and_no_launch_is_too_large():
         text = "\n".join(" ".join(map(str, c)) for c in cases + big)
         lines = subprocess.run([exe], input=text, capture_output=True, text=True, check=True).stdout.split("\n")
     got = [tuple(map(int, l.split())) for l in lines if l]
-    tile, target, split, most = got.pop()
+    tile, target, split, most, shared = got.pop()
     assert most == 1 << 26
     for c, (rows, n, lens), (has_long, limit, group_limit, items) in zip(cases, batches, got):
         if not has_long:
@@ -185,9 +185,14 @@ def test_there_is_a_workgroup_for_every_item_and_no_launch_is_too_large():
         r = rows * group
         limits = np.where(np.arange(len(rows)) < n, limit, group_limit)
         tiles = np.where(r > limits, -(-r // tile), 0)
-        work = float((tiles * lens).sum()) * kv * 1.25 / target
-        chunk = split if work < split else (int(work) + 128) >> 7 << 7
+        whole, half = float((tiles * lens).sum()) * kv, 0.5 * float(tiles.sum()) * kv
+        each = whole / max(shared - half, 0.5 * shared)
+        if each < split:
+            each = whole / max(target - half, 0.5 * target)
+        chunk = split if each < split else (int(each) + 128) >> 7 << 7
         cuts = np.where(lens <= chunk, 1, -(-lens // chunk))
         assert int((tiles * cuts).sum()) * kv <= items, c
+        # partial results: of cut tiles only
+        assert int((tiles * cuts)[cuts > 1].sum()) * kv <= 2 * shared, c
     for c, g in zip(big, got[len(cases):]):
         assert 0 < g[3] * 256 < 1 << 32, (c, g)
