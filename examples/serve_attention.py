@@ -2,7 +2,7 @@
 LoRA updates of q, k, v and o, rotary positions, a paged cache and attention over it, with prompts in
 chunks beside decoding users, forks, sequences that end, and a compaction.
 
-    python examples/serve_attention.py [--steps 12] [--check]
+    python examples/serve_attention.py [--steps 12] [--check] [--answers 5]
 
 Every step is the same few calls for all users together:
     lora_kv_plan, lora_kv_copy_pages        who continues what, and room for the new rows
@@ -11,6 +11,12 @@ Every step is the same few calls for all users together:
                 lora_rope_append            q rotated, k rotated into its page, v into its page
                 lora_kv_attention           new rows over all of their sequence
                 lora_apply                  the output projection's update on top of its base product
+--answers N draws N answers to each of a few prompts instead, token by token: the prompts fork, and every step is
+    lora_kv_plan, lora_kv_copy_pages, lora_kv_share
+    per layer:  lora_add_norm                   the residual stream takes the layer before, and is normalised for the next products
+                base products, LoRA updates and lora_rope_append as above
+                lora_kv_attention_shared        a prompt's pages are read once for all of its answers
+    lora_add_norm, the product with the vocabulary, lora_sample
 --check recomputes every sequence from its first token in 64 bits, exactly and with the loop's roundings to bf16, and
 compares how far the loop and the rounded recomputation are from the exact one.
 """
@@ -111,8 +117,109 @@ class Server:
         return x
 
 
-def recompute(model: Layers, x, adapter, freq, rounded: bool):
-    """One sequence from its first token, in 64 bits on the CPU; rounded: to bf16 wherever the loop above holds bf16."""
+class Answers(Server):
+    """A server that draws tokens: slots 0 .. prompts - 1 hold the prompts, the others their answers."""
+
+    def __init__(self, model: Layers, vocab=1003, seed=0, **kw):
+        super().__init__(model, **kw)
+        g = torch.Generator().manual_seed(seed + 1)
+        m, rand = model, lambda *s: torch.randn(s, generator=g)                                   # noqa: E731
+        self.vocab = vocab
+        self.embed = rand(vocab, m.hidden).to(torch.bfloat16).cuda()
+        self.head = (rand(m.hidden, vocab) * (3.0 / math.sqrt(m.hidden))).to(torch.bfloat16).cuda()
+        self.gains = [(1.0 + 0.2 * rand(m.hidden)).to(torch.bfloat16).cuda() for _ in range(m.n_layers + 1)]
+        self.norms = [L.Norm(w, eps=1e-6) for w in self.gains]
+
+    def logits(self, tokens, rows):
+        """tokens: the new ones, slot after slot, rows[s] of slot s, on the device.  Logits of every such slot's last row."""
+        m, P, state = self.model, tokens.shape[0], self.states[0]
+        start = torch.from_numpy(np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)).cuda()
+        batch = L.KvBatch(start, state.seq_len, state.table, n_rows=P, max_rows=max(rows))
+        shared = L.KvShared(self.slots, P)
+        L.lora_kv_share(self.cache, batch, shared, max_rows=16)
+        ids = torch.from_numpy(np.repeat(self.adapter, rows).astype(np.int32)).cuda()
+        seg = L.Segments(P)
+        ws = torch.empty(max(L.lora_group_ws_bytes(m.pool, 0, 3, P), L.lora_v_bytes(m.pool, 3, P), 256), dtype=torch.uint8, device="cuda")
+        aws = torch.empty(L.lora_kv_attention_shared_ws_bytes(self.cache, batch, shared, m.heads), dtype=torch.uint8, device="cuda")
+        wq, wk, _ = m.widths
+        h, y, x = self.embed[tokens.long()], None, torch.empty((P, m.hidden), dtype=torch.bfloat16, device="cuda")
+        for layer in range(m.n_layers):
+            L.lora_add_norm(self.norms[layer], P, h, m.hidden, y, m.hidden, h, m.hidden, x, m.hidden)      # h += y in place
+            qkv = x @ m.wqkv[layer]
+            q, k, v = qkv, qkv[:, wq:], qkv[:, wq + wk:]
+            ld = qkv.shape[1]
+            if layer == 0:
+                L.lora_build_apply_group(m.pool, 0, 0, x, m.hidden, None, ids, None, P, seg, [q, k, v], [ld] * 3, ws)
+            else:
+                L.lora_apply_group(m.pool, layer, 0, x, m.hidden, None, seg, [q, k, v], [ld] * 3, ws)
+            L.lora_rope_append(self.cache, layer, batch, self.rope, q, ld, k, ld, v, ld, q, ld, m.heads)
+            out = torch.empty((P, wq), dtype=torch.bfloat16, device="cuda")
+            L.lora_kv_attention_shared(self.cache, layer, batch, shared, q, ld, m.heads, out, wq, None, 1.0 / math.sqrt(m.dim), aws)
+            y = out @ m.wo[layer]
+            L.lora_apply(m.pool, layer, 3, out, wq, None, seg, y, m.hidden, ws)
+        L.lora_add_norm(self.norms[-1], P, h, m.hidden, y, m.hidden, None, 0, x, m.hidden)
+        self.status, self.spared = batch.status, shared.counts
+        last = (start[1:] - 1)[start[1:] > start[:-1]].long()
+        return x[last] @ self.head
+
+    def draw(self, logits, how, u):
+        token = torch.empty(logits.shape[0], dtype=torch.int32, device="cuda")
+        L.lora_sample(logits, self.vocab, logits.shape[0], self.vocab, how, u, token, dtype=L.LORA_DTYPE_BF16)
+        return token
+
+
+def answer(prompts=3, width=5, steps=12, seed=0, check=False):
+    """Draws `width` answers of `steps` tokens to each of a few prompts.  With check: the error of the logits as a multiple of what
+    the roundings make, and for every draw the logits, the settings, the random numbers and the tokens."""
+    rng = np.random.default_rng(seed)
+    model = Layers(seed=seed)
+    server = Answers(model, seed=seed, slots=prompts * (width + 1))
+    slots, of = server.slots, [s % prompts for s in range(prompts * (width + 1))]
+    text = [rng.integers(0, server.vocab, int(rng.integers(20, 150))).tolist() if s < prompts else [] for s in range(slots)]
+    rows = [len(t) for t in text]
+    server.plan([-1] * slots, rows)
+    for s in range(prompts):
+        server.adapter[s] = int(rng.integers(-1, 5))
+    dev = lambda a, t: torch.from_numpy(np.asarray(a, t)).cuda()                                  # noqa: E731
+    # the answers have temperatures and limits of their own
+    n = slots - prompts
+    settings = dict(temperature=rng.choice([0.0, 0.7, 1.0, 1.3], n), top_k=rng.choice([0, 40, 5], n), top_p=rng.choice([1.0, 0.9, 0.6], n), min_p=rng.choice([0.0, 0.05], n))
+    how = L.Sampling(*(dev(settings[f], np.int32 if f == "top_k" else np.float32) for f in ("temperature", "top_k", "top_p", "min_p")))
+    logits = server.logits(dev(sum(text, []), np.int64), rows)[dev([of[s] for s in range(prompts, slots)], np.int64)].contiguous()
+    drawn, off, rounding = [], 0.0, 0.0
+    for step in range(steps):
+        u = rng.random(n).astype(np.float32)
+        token = server.draw(logits, how, dev(u, np.float32))
+        if check:
+            drawn.append((logits.float().cpu().numpy(), settings, u, token.cpu().numpy()))
+        # at first all answers fork from their prompts, which stay as they are
+        src = [s if s < prompts or step else of[s] for s in range(slots)]
+        before = [server.length[p] for p in src]
+        server.plan(src, [b + (s >= prompts) for s, b in enumerate(before)])
+        if step % 5 == 4:
+            server.compact()
+        logits = server.logits(token, [0] * prompts + [1] * n)
+        for s, t in zip(range(prompts, slots), token.tolist()):
+            text[s] = (text[of[s]] if step == 0 else text[s]) + [t]
+        groups, _, members, spared = server.spared.tolist()
+        assert int(server.moves.status) == 0 and int(server.status) == 0
+        line = f"step {step}: {n} answers, {members} of them in {groups} groups, {spared} tokens read once less"
+        if check:
+            freq = L.lora_rope_freqs(model.dim, scaling=L.LORA_ROPE_PARTS, factor=4.0, original_len=128.0, low=1.0, high=8.0)
+            for s in range(prompts, slots):
+                x = server.embed.cpu()[text[s]]
+                exact, same = (recompute(model, x, server.adapter[s], freq, rounded, server)[-1] for rounded in (False, True))
+                got = logits[s - prompts].double().cpu()
+                off += float((got - exact).square().sum())
+                rounding += float((same - exact).square().sum())
+            line += f", error {(off / rounding) ** 0.5:.2f} times what rounding to bf16 makes"
+        print(line, flush=True)
+    return ((off / rounding) ** 0.5 if rounding else 0.0), drawn
+
+
+def recompute(model: Layers, x, adapter, freq, rounded: bool, answers=None):
+    """One sequence from its first token, in 64 bits on the CPU; rounded: to bf16 wherever the loop above holds bf16.  answers: with its
+    norms, and up to the logits."""
     m, r = model, (lambda t: t.to(torch.bfloat16).double()) if rounded else (lambda t: t)
     n = x.shape[0]
     turn = torch.polar(torch.ones(n, m.dim // 2, dtype=torch.float64), torch.arange(n).double()[:, None] * torch.tensor(freq, dtype=torch.float64))
@@ -129,16 +236,24 @@ def recompute(model: Layers, x, adapter, freq, rounded: bool):
         z = torch.complex(t[:, :, 0], t[:, :, 1]) * turn[:, None]
         return r(torch.stack([z.real, z.imag], 2).view(n, heads, m.dim))
 
+    def norm(layer):
+        if answers is None:
+            return x
+        return r(x / (x.square().mean(1, keepdim=True) + 1e-6).sqrt() * answers.gains[layer].cpu().double())
+
     for layer in range(m.n_layers):
-        qkv = torch.split(r(x @ m.wqkv[layer].cpu().double()), m.widths, dim=1)
-        q, k, v = (r(t + lora(layer, j, x)) for j, t in enumerate(qkv))
+        inp = norm(layer)
+        qkv = torch.split(r(inp @ m.wqkv[layer].cpu().double()), m.widths, dim=1)
+        q, k, v = (r(t + lora(layer, j, inp)) for j, t in enumerate(qkv))
         q, k, v = turned(q, m.heads), turned(k, m.kv), v.view(n, m.kv, m.dim)
         k, v = (t.repeat_interleave(m.heads // m.kv, 1).transpose(0, 1).contiguous() for t in (k, v))
         s = torch.matmul(q.transpose(0, 1), k.transpose(1, 2).contiguous()) / math.sqrt(m.dim)
         s = s.masked_fill(torch.ones(n, n, dtype=torch.bool).triu(1), -math.inf)
         out = r(torch.matmul(torch.softmax(s, -1), v).transpose(0, 1).reshape(n, -1))
-        x = r(x + r(r(out @ m.wo[layer].cpu().double()) + lora(layer, 3, out)))
-    return x
+        y = r(r(out @ m.wo[layer].cpu().double()) + lora(layer, 3, out))
+        # (the last norm takes the sum as it is)
+        x = x + y if answers is not None and layer == m.n_layers - 1 else r(x + y)
+    return x if answers is None else r(norm(-1) @ answers.head.cpu().double())
 
 
 def main(argv=None):
@@ -147,7 +262,10 @@ def main(argv=None):
     ap.add_argument("--steps", type=int, default=12)
     ap.add_argument("--check", action="store_true")
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--answers", type=int, default=0)
     args = ap.parse_args(argv)
+    if args.answers:
+        return answer(width=args.answers, steps=args.steps, seed=args.seed, check=args.check)[0], 0.0
     rng = np.random.default_rng(args.seed)
     model = Layers(seed=args.seed)
     server = Server(model)

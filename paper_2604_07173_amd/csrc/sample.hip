@@ -456,12 +456,12 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
     Border border{endless ? INFINITY : -INFINITY, endless ? 0xFFFFFFFFu : 0u};
     const bool by_k = k_most > 0 && k_most < p.vocab && !endless, by_p = top_p < 1.f && !endless;
     unsigned listed = 0, lo = 0, hi = 0;
+    bool in_list = false;                 // all tokens down to top_k's border are listed
     // 2: the first k of the order
     if (by_k) {
         const u64 want = (u64)k_most;
         const float per = (float)FINE / (top - low);
-        bool in_list = false;
-        if (k_most <= Lds::FEW / 2 && low > -INFINITY && low < top && per < 1e30f) {
+        if (k_most <= THREADS / 4 * 3 && low > -INFINITY && low < top && per < 1e30f) {
             // bins of the threads' largest, from the row's down to the least of them
             sh.fine.count[tid] = 0;
             __syncthreads();
@@ -471,9 +471,9 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
             // tokens of that bin and of those before it: by the same function, so that none of the k is missed
             const float end = sh.bin == FINE - 1 ? INFINITY : (float)(sh.bin + 1);
             listed = list(no, [&](float l) { return (top - l) * per < end; }, lo, hi);
-            in_list = listed <= Lds::FEW;
+            in_list = listed <= Lds::LISTED;
         }
-        if (in_list) {
+        if (in_list && listed <= Lds::FEW) {
             // `side` neighbouring threads per token, each for every side-th of the others
             int shift = 0;
             while ((listed << (shift + 1)) <= THREADS && shift < 6) ++shift;
@@ -515,20 +515,25 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
             if (lead && keep && before <= goal && goal < before + own) chosen(number_in(entry), of_key(key_in(entry)), total);
             return;
         }
-        for (int i = tid; i < COUNTS; i += THREADS) sh.count[i] = 0;
-        __syncthreads();
-        each(some, [&](float l, int) {
-            const int b = weigh.bin(l, by_number);
-            if (b < COUNTS) atomicAdd(&sh.count[b], 1u);
-        });
-        __syncthreads();
-        unsigned own[COUNTS / THREADS];
+        const auto all = [](float) { return true; };
+        if (in_list) {
+            border = refine(no, all, lo, hi, listed, want, 0);
+        } else {
+            for (int i = tid; i < COUNTS; i += THREADS) sh.count[i] = 0;
+            __syncthreads();
+            each(some, [&](float l, int) {
+                const int b = weigh.bin(l, by_number);
+                if (b < COUNTS) atomicAdd(&sh.count[b], 1u);
+            });
+            __syncthreads();
+            unsigned own[COUNTS / THREADS];
 #pragma unroll
-        for (int k = 0; k < COUNTS / THREADS; ++k) own[k] = sh.count[tid * (COUNTS / THREADS) + k];
-        find_bin(sh, own, want);
+            for (int k = 0; k < COUNTS / THREADS; ++k) own[k] = sh.count[tid * (COUNTS / THREADS) + k];
+            find_bin(sh, own, want);
+        }
         // a border behind the bins cuts nothing that has a weight; but where T is so small that they are of no use all tokens are there
         const bool useless = !(by_number.each < INFINITY);
-        if (sh.bin >= 0 || useless) {
+        if (!in_list && (sh.bin >= 0 || useless)) {
             const int bin = sh.bin < 0 ? COUNTS : sh.bin;
             const u64 above = sh.before;
             const Weigh::Bin it = weigh.only(by_number, bin);
@@ -543,7 +548,20 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
     unsigned c = 0;
     bool summed = false;
     // 3: the border of top_p
-    if (by_p) {
+    if (in_list) {
+        summed = true;                    // nothing that is kept is not listed
+        if (by_p) {
+            u64 left = 0;
+            for (unsigned i = tid; i < listed; i += THREADS) {
+                const float l = of_key(key_in(sh.list[i]));
+                if (l > border.value) left += weigh.mass(l);
+            }
+            const u64 above = sum_of(left), tie = weigh.mass(border.value), want = part_of(above + tie * border.ties);
+            const auto all = [](float) { return true; };
+            if (want > above) border.ties = (unsigned)((want - above + tie - 1) / tie);
+            else border = refine(yes, all, key_of(border.value) + 1, hi, listed, want, 0);
+        }
+    } else if (by_p) {
         u64 tail = 0;                     // weights behind the bins
         __syncthreads();
         for (int i = tid; i < WAVES * BINS; i += THREADS) sh.mass[0][i] = 0;
@@ -633,7 +651,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
             const u64 entry = sh.list[i];
             const float l = of_key(key_in(entry));
             const int w = (number_in(entry) + row.skew) / VEC / (steps * 64);
-            if (l > border.value) atomicAdd(&sh.wave_kept[w], weigh.mass(l));
+            if (l > border.value) atomicAdd(&sh.wave_kept[w], weigh.kept(l));
             else if (l == border.value) atomicAdd(&sh.wave_count[w], 1u);
         }
         __syncthreads();

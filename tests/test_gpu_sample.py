@@ -108,6 +108,17 @@ def test_every_row_has_its_own_rule():
           least=rng.choice([0.0, 0.01, 0.3], R), u=us(R, 9))
 
 
+@pytest.mark.parametrize("V,k", [(5000, 65), (5000, 190), (20000, 257), (20000, 600), (20000, 768), (20000, 769), (60000, 4000)])
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+def test_lists_of_all_lengths(V, k, kind):
+    """Lists that are compared in pairs, counted in bins, and none at all, with every other limit on top."""
+    for i, rule in enumerate((dict(), dict(p=0.7), dict(p=0.999), dict(least=0.02), dict(p=0.9, least=0.001, T=1.4), dict(T=0.4, p=0.5), dict(T=30.0, p=0.9))):
+        check(logits(6, V, kind, seed=i), u=us(6, i), k=k, **rule)
+    x = logits(6, V, kind)
+    x[:, : V // 3] = 4.0                              # equal ones, more than a list takes
+    check(x, u=us(6), k=k, p=0.8)
+
+
 def test_all_of_u():
     """One row's tokens over a fine grid of u, the ends among it."""
     R = 500
