@@ -41,9 +41,17 @@ constexpr int kArrays = S ? kSharedArrays : kPlanArrays;
 template <bool S>
 constexpr int kInlineWords = kPlanHead + kArrays<S> * kMostInline<S>;
 
+template <bool S>
 struct Seq {
     int row0, rows, len, pos0;           // first new row and their number, length, position of the first new row
-    int first;                           // first token, 0 where nothing is shared
+    static constexpr int first = 0;
+    static constexpr bool group = false;
+};
+
+template <>
+struct Seq<true> {
+    int row0, rows, len, pos0;
+    int first;                           // first token
     bool group;                          // of rows that share tokens; row0 counts in the list of such rows then
 };
 
@@ -55,26 +63,28 @@ __device__ inline int place_in_groups(const AttnParams &p, int s, int rows)
 }
 
 template <bool S>
-__device__ inline Seq seq_of(const AttnParams &p, int s)
+__device__ inline Seq<S> seq_of(const AttnParams &p, int s)
 {
     const KvRows &b = p.b;
-    Seq q;
-    q.group = S && s < p.g.most;
-    if (q.group) {
-        const int32_t *g = p.g.groups + 4 * (int64_t)s;
-        q.row0 = min(max(0, g[2]), p.g.most_rows);
-        q.rows = (unsigned)g[0] < (unsigned)b.n_seqs ? min(max(0, g[3]), p.g.most_rows - q.row0) : 0;
-        q.len = min(max(0, g[1]), b.tokens_max);
-        q.pos0 = q.len;                   // every row sees all of them
-        q.first = 0;
-        return q;
+    Seq<S> q;
+    if constexpr (S) {
+        q.group = s < p.g.most;
+        if (q.group) {
+            const int32_t *g = p.g.groups + 4 * (int64_t)s;
+            q.row0 = min(max(0, g[2]), p.g.most_rows);
+            q.rows = (unsigned)g[0] < (unsigned)b.n_seqs ? min(max(0, g[3]), p.g.most_rows - q.row0) : 0;
+            q.len = min(max(0, g[1]), b.tokens_max);
+            q.pos0 = q.len;               // every row sees all of them
+            q.first = 0;
+            return q;
+        }
+        s -= p.g.most;
     }
-    if (S) s -= p.g.most;
     q.row0 = min(max(0, b.row_start[s]), b.n_rows);
     q.rows = max(0, min(b.row_start[s + 1], b.n_rows) - q.row0);
     q.len = min(max(0, b.seq_len[s]), b.tokens_max);
     q.pos0 = q.len - q.rows;
-    q.first = S && place_in_groups(p, s, q.rows) >= 0 ? min(p.g.own[s], max(0, q.pos0)) : 0;
+    if constexpr (S) q.first = place_in_groups(p, s, q.rows) >= 0 ? min(p.g.own[s], max(0, q.pos0)) : 0;
     return q;
 }
 
@@ -88,14 +98,14 @@ __device__ inline int slot_of(const AttnParams &p, int s)
 
 // The batch's row of the plan's row `at` of such a sequence.
 template <bool S>
-__device__ inline int row_at(const AttnParams &p, const Seq &q, int at)
+__device__ inline int row_at(const AttnParams &p, const Seq<S> &q, int at)
 {
     return S && q.group ? (int)min((unsigned)p.g.rows[at], (unsigned)p.b.n_rows - 1u) : at;
 }
 
 // Where a finished row goes: its place in whole_o (by heads), or -1 for the output itself.
 template <bool S>
-__device__ inline int64_t whole_at(const AttnParams &p, const Seq &q, int s, int i)
+__device__ inline int64_t whole_at(const AttnParams &p, const Seq<S> &q, int s, int i)
 {
     if (!S) return -1;
     if (q.group) return q.row0 + i;
@@ -114,8 +124,8 @@ __device__ inline void note(const AttnParams &p, int64_t row, int qh, int first,
 }
 
 // Tiles that the sequence has of this kind.
-template <Kind K>
-__device__ inline int tiles_of(const AttnParams &p, const Seq &q)
+template <Kind K, bool S>
+__device__ inline int tiles_of(const AttnParams &p, const Seq<S> &q)
 {
     const int n = q.rows * p.group;
     if ((n <= (q.group ? p.group_limit : p.short_limit)) != (K == kShort)) return 0;
@@ -123,8 +133,8 @@ __device__ inline int tiles_of(const AttnParams &p, const Seq &q)
 }
 
 // Most tokens that a tile of the sequence sees.
-template <Kind K>
-__device__ inline int reach_of(const AttnParams &p, const Seq &q)
+template <Kind K, bool S>
+__device__ inline int reach_of(const AttnParams &p, const Seq<S> &q)
 {
     if (!p.window) return q.len - q.first;
     const int most = p.window - 1 + min(q.rows, tile_rows<K>(p) / p.group_div + 2);
@@ -148,8 +158,8 @@ struct Range {
     int lo, hi;
 };
 
-template <Kind K>
-__device__ inline Range range_of(const AttnParams &p, const Seq &q, int tile)
+template <Kind K, bool S>
+__device__ inline Range range_of(const AttnParams &p, const Seq<S> &q, int tile)
 {
     const int R = tile_rows<K>(p);
     const int i0 = tile * R / p.group_div, i1 = min(q.rows - 1, (tile * R + R - 1) / p.group_div);
@@ -184,7 +194,8 @@ __device__ inline int cut_of(const Range &r, int splits)
 }
 
 // What a sequence adds to the plan's arrays.
-__device__ inline void plan_entry(const AttnParams &p, const Seq &q, int shift, int chunk, int (&own)[kPlanSums])
+template <bool S>
+__device__ inline void plan_entry(const AttnParams &p, const Seq<S> &q, int shift, int chunk, int (&own)[kPlanSums])
 {
     const int tiles = tiles_of<kLong>(p, q);
     const int cuts = splits_of(reach_of<kLong>(p, q), chunk);
@@ -211,7 +222,7 @@ __device__ inline int group_rows(const AttnParams &p, bool no_rows)
 }
 
 template <bool S>
-__device__ inline void store_seq(int32_t *plan, int64_t n_seqs, int s, const Seq &q)
+__device__ inline void store_seq(int32_t *plan, int64_t n_seqs, int s, const Seq<S> &q)
 {
     if (S) plan[kPlanHead + kSeqFirst * n_seqs + s] = q.first;
     plan[kPlanHead + kSeqRow0 * n_seqs + s] = q.row0;
@@ -220,15 +231,17 @@ __device__ inline void store_seq(int32_t *plan, int64_t n_seqs, int s, const Seq
 }
 
 template <bool S>
-__device__ inline Seq planned_seq(const AttnParams &p, const int32_t *plan, int s)
+__device__ inline Seq<S> planned_seq(const AttnParams &p, const int32_t *plan, int s)
 {
     const int64_t n_seqs = plan_seqs<S>(p);
-    Seq q;
+    Seq<S> q;
     q.row0 = uniform(plan[kPlanHead + kSeqRow0 * n_seqs + s]);
     q.rows = uniform(plan[kPlanHead + kSeqRows * n_seqs + s]);
     q.len = uniform(plan[kPlanHead + kSeqLen * n_seqs + s]);
-    q.group = S && s < p.g.most;
-    q.first = S ? uniform(plan[kPlanHead + kSeqFirst * n_seqs + s]) : 0;
+    if constexpr (S) {
+        q.group = s < p.g.most;
+        q.first = uniform(plan[kPlanHead + kSeqFirst * n_seqs + s]);
+    }
     q.pos0 = q.group ? q.len : q.len - q.rows;
     return q;
 }
@@ -256,13 +269,13 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
 {
     constexpr int MOST = kMostInline<S> / 64;
     const int lane = threadIdx.x & 63, n = plan_seqs<S>(p), each = (n + 63) >> 6;
-    Seq q[MOST];
+    Seq<S> q[MOST];
     unsigned bad = 0;
     float work = 0.f;
 #pragma unroll
     for (int k = 0; k < MOST; ++k) {
         const int s = lane * each + k;
-        q[k] = Seq{0, 0, 0, 0, 0, false};
+        q[k] = Seq<S>{};
         if (k < each && s < n) {
             q[k] = seq_of<S>(p, s);
             bad |= plan_faults_of<S>(p, s);
@@ -341,7 +354,7 @@ struct Place {
 };
 
 template <bool S>
-__device__ inline Place place_of(const AttnParams &p, const int32_t *plan, int unit, Seq &q)
+__device__ inline Place place_of(const AttnParams &p, const int32_t *plan, int unit, Seq<S> &q)
 {
     const int32_t *base = plan + kPlanHead + kBaseUnit * plan_seqs<S>(p);
     Place x;

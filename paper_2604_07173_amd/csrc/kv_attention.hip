@@ -42,7 +42,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
     float work = 0.f, units = 0.f, tiles = 0.f;
     unsigned bad = 0;
     for (int s = tid; s < n; s += kPlanThreads) {
-        const Seq q = seq_of<S>(p, s);
+        const Seq<S> q = seq_of<S>(p, s);
         bad |= plan_faults_of<S>(p, s);
         work += (float)tiles_of<kLong>(p, q) * (float)reach_of<kLong>(p, q);
         if (S) tiles += (float)tiles_of<kLong>(p, q);
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
         const int s = s0 + tid;
         int own[kPlanSums] = {}, upto[kPlanSums];
         if (s < n) {
-            const Seq q = seq_of<S>(p, s);
+            const Seq<S> q = seq_of<S>(p, s);
             if (!no_rows) plan_entry(p, q, shift, chunk, own);
             store_seq<S>(p.plan, n, s, q);
         }
@@ -136,20 +136,21 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
     // A tile of the stretch, or the part of one: its rows, and its tokens [lo, hi).  Q's rows and the first page number are
     // on their way before the tile before is written.
     struct Part {
-        Seq q;
+        Seq<S> q;
         int s, head, tile, lo, hi, units;
-        int parts;                        // of the tile, if this one begins it, else 0
         bool whole, later;                // later: not the stretch's first tile
     } part;
+    int parts = 0;                        // S: of the tile, if this part begins it, else 0
     int see_lo[MT], see_hi[MT], all_lo, all_hi, page = 0;
     bf16x8 qf[MT][KS];
     const auto take = [&](int u) {
-        Seq q;
+        Seq<S> q;
         const Place pl = place_of<S>(p, plan, u, q);
         const int k0 = u - pl.start, k1 = min(pl.units, k0 + end - u), tile = pl.tile, head = pl.head;
         const Range rg = range_of<kShort>(p, q, tile);
         const int lo = rg.lo + (k0 << unit_shift), hi = k1 == pl.units ? rg.hi : min(rg.hi, rg.lo + (k1 << unit_shift));
-        part = Part{q, pl.s, head, tile, lo, hi, k1 - k0, S && k0 == 0 ? (u + pl.units - 1) / share - (int)blockIdx.x + 1 : 0, k1 - k0 == pl.units, u != first};
+        part = Part{q, pl.s, head, tile, lo, hi, k1 - k0, k1 - k0 == pl.units, u != first};
+        if (S) parts = k0 == 0 ? (u + pl.units - 1) / share - (int)blockIdx.x + 1 : 0;
         if (lo < hi) page = (p.b.table + (int64_t)slot_of<S>(p, pl.s) * p.b.max_pages)[min(lo + wave * kBlock + (lane & 31), hi - 1) >> p.c.page_shift];
         // this lane's rows
 #pragma unroll
@@ -159,7 +160,8 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
             const bool real = r < q.rows * p.group;
             see_hi[mt] = !real ? 0 : p.causal ? min(hi, q.pos0 + i + 1) : hi;
             see_lo[mt] = p.window ? max(lo, q.pos0 + i - p.window + 1) : lo;
-            const uint16_t *from = p.q + (int64_t)(real ? row_at<S>(p, q, q.row0 + i) : 0) * p.ldq + (head * p.group + g) * D;
+            const int at = S ? real ? row_at<S>(p, q, q.row0 + i) : 0 : q.row0 + i;
+            const uint16_t *from = p.q + (int64_t)at * p.ldq + (head * p.group + g) * D;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const int d = ks * 32 + grp * 8;
@@ -307,6 +309,7 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
         }
         if (bad) atomicOr(p.b.status, LORA_STATUS_BAD_PAGE);
         const Part done = part;
+        const int begins = parts;
         const int64_t slot = 2 * blockIdx.x + done.later;      // of a part's results: the stretch's first tile, or its last
         if (u < end) take(u);
         // the four waves' parts of the range, 16 rows at a time
@@ -334,13 +337,26 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
                     total += f[w] * s_l[w][row];
                 }
                 const int i = r / p.group_div;
-                const int64_t t = row_at<S>(p, done.q, done.q.row0 + i);
+                int64_t t = done.q.row0 + i;
                 const int qh = head * p.group + r - i * p.group;
-                // parts of cut tiles and, where tokens are shared, of rows of groups
-                const int64_t group_row = whole_at<S>(p, done.q, done.s, i), both = done.whole ? group_row : -1;
-                const bool final = done.whole && both < 0;
-                const int64_t at = both < 0 ? slot * R + mt * 16 + row : both * p.heads + qh;
-                float *part_o = both < 0 ? p.part_o : p.whole_o, *part_ml = both < 0 ? p.part_ml : p.whole_ml;
+                int64_t at = slot * R + mt * 16 + row;
+                bool final = done.whole;
+                float *part_o = p.part_o, *part_ml = p.part_ml;
+                if constexpr (S) {            // parts of cut tiles stay, and so does all that is a group's rows'
+                    const int64_t group_row = whole_at<S>(p, done.q, done.s, i);
+                    t = row_at<S>(p, done.q, done.q.row0 + i);
+                    if (begins && group_row >= 0 && (threadIdx.x & 15) == 0) {
+                        const int next = (int)((2 * ((int64_t)blockIdx.x + 1)) * R + mt * 16 + row);
+                        if (final) note(p, group_row, qh, (int)(group_row * p.heads + qh), 0, 1, kFoundWhole);
+                        else note(p, group_row, qh, (int)at, next, begins, kFoundShort);
+                    }
+                    if (final && group_row >= 0) {
+                        at = group_row * p.heads + qh;
+                        part_o = p.whole_o;
+                        part_ml = p.whole_ml;
+                        final = false;
+                    }
+                }
                 const float norm = total == 0.f ? 0.f : 1.f / total;
                 for (int d = (threadIdx.x & 15) * 4; d < D; d += 64) {
                     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -357,10 +373,6 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
                     }
                 }
                 if ((threadIdx.x & 15) == 0) {
-                    if (S && done.parts && group_row >= 0) {
-                        const int next = (int)((2 * ((int64_t)blockIdx.x + 1)) * R + mt * 16 + row);
-                        note(p, group_row, qh, (int)at, next, done.parts, both < 0 ? kFoundShort : kFoundWhole);
-                    }
                     if (!final) {
                         part_ml[at * 2] = top;
                         part_ml[at * 2 + 1] = total;
@@ -458,25 +470,24 @@ __device__ inline void join_found(const AttnParams &p, RowSum &x, int4 f)
     join_add<DP>(p, x, ml, o, n, [&](int c) { return (int64_t)min((unsigned)(c == 0 ? f.x : f.y + (c - 1) * by), room - 1u); });
 }
 
-// Joins the parts of short tiles that lie across the ends of workgroups' stretches: join_rows workgroups per such end, those of the first
-// one inside a tile do it.  Workgroups behind these, join_long of them: the rows of cut long tiles, a wave per row and head.  Where
+// Joins the parts of short tiles that lie across the ends of workgroups' stretches: a workgroup per such end, the first
+// one inside a tile does it.  Workgroups from join_blocks on, join_long of them: the rows of cut long tiles, a wave per row and head.  Where
 // tokens are shared, those behind: the rows of groups, a wave per row and head, over the shared tokens and over their own.
 template <int DP, bool S>
 __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
 {
     const int32_t *plan = p.plan;        // the kernels before have left it
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int block = blockIdx.x - p.join_blocks * p.join_rows;
-    if (block < 0) {
-        const int share = uniform(plan[kShare]), b = blockIdx.x / p.join_rows, y = blockIdx.x - b * p.join_rows, cut = (b + 1) * share;
+    if ((int)blockIdx.x < p.join_blocks) {
+        const int share = uniform(plan[kShare]), b = blockIdx.x, cut = (b + 1) * share;
         if (cut >= plan[kUnits]) return;
-        Seq q;
+        Seq<S> q;
         const Place pl = place_of<S>(p, plan, cut, q);
         if (pl.start == cut || pl.start < b * share) return;       // between two tiles, or not the first end inside this one
         if (S && whole_at<S>(p, q, pl.s, 0) >= 0) return;          // of a group
         const int n = (pl.start + pl.units - 1) / share - b + 1;
         const int rows = min(1 << p.short_shift, q.rows * p.group - (pl.tile << p.short_shift));
-        for (int row = y * 4 + wave; row < rows; row += 4 * p.join_rows) {
+        for (int row = blockIdx.y * 4 + wave; row < rows; row += 4 * gridDim.y) {
             const int r = (pl.tile << p.short_shift) + row, i = r / p.group_div;
             RowSum x;
             join_add<DP>(p, x, p.part_ml, p.part_o, n, [&](int c) { return short_part(p, b, c, pl.start, share, row); });
@@ -484,10 +495,11 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         }
         return;
     }
-    const int seqs = plan_seqs<S>(p);
+    if (blockIdx.y) return;
+    const int seqs = plan_seqs<S>(p), block = blockIdx.x - p.join_blocks;
     if (S && block >= p.join_long) {
         const int n = plan[kGroupRows] * p.heads;
-        for (int u = (block - p.join_long) * 4 + wave; u < n; u += (gridDim.x - p.join_blocks * p.join_rows - p.join_long) * 4) {
+        for (int u = (block - p.join_long) * 4 + wave; u < n; u += (gridDim.x - p.join_blocks - p.join_long) * 4) {
             const int4 a = p.found[u], b = p.found[u + p.g.most_rows * p.heads];
             const int v = u / p.heads_div, t = min((unsigned)p.g.rows[v], (unsigned)p.b.n_rows - 1u);
             RowSum x;
@@ -501,7 +513,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
     const int units = plan[kJoinUnits], chunk = plan[kChunk];
     for (int u = block * 4 + wave; u < units; u += p.join_long * 4) {
         const int s = seq_at<S>(p, base, u);
-        const Seq q = planned_seq<S>(p, plan, s);
+        const Seq<S> q = planned_seq<S>(p, plan, s);
         const int left = u - base[s];
         const int i = left / p.heads_div, qh = left - i * p.heads;
         const int head = qh / p.group_div;
@@ -556,8 +568,7 @@ hipError_t launch_short_and_join(AttnParams &p, const Kinds &k, int64_t reach, i
     p.join_long = k.has_long && reach > kLongMinSplit ? 1024 : 0;
     p.join_blocks = k.has_short && reach > 1 << kUnitShift ? (int)grid - 1 : 0;
     if (p.join_blocks + p.join_long + shared > 0) {
-        p.join_rows = (join_rows + 3) / 4;
-        const dim3 both(p.join_blocks * p.join_rows + p.join_long + shared), block(256);
+        const dim3 both(p.join_blocks + p.join_long + shared, (join_rows + 3) / 4), block(256);
         if (p.c.dim <= 64) hipLaunchKernelGGL((join_kernel<64, S>), both, block, 0, s, p);
         else if (p.c.dim <= 128) hipLaunchKernelGGL((join_kernel<128, S>), both, block, 0, s, p);
         else hipLaunchKernelGGL((join_kernel<256, S>), both, block, 0, s, p);

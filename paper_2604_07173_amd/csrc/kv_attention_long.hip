@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     // the cuts of a tile lie n_heads apart, tiles behind each other, those with the longest ranges first
     const int32_t *base = plan + kPlanHead + kBaseItem * plan_seqs<S>(p);
     const int seq = seq_at<S>(p, base, n);
-    const Seq q = planned_seq<S>(p, plan, seq);
+    const Seq<S> q = planned_seq<S>(p, plan, seq);
     const int left = uniform(n - base[seq]);
     const int pair = left / p.kv_div, head = left - pair * p.c.n_heads;
     const int chunk = uniform(plan[kChunk]);
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     const int r = r0 + col;
     const int i = r / p.group_div, g = r - i * p.group;
     const bool real = r < n_rows;
-    const int64_t t = real ? row_at<S>(p, q, q.row0 + i) : 0;
+    const int64_t t = S ? real ? row_at<S>(p, q, q.row0 + i) : 0 : q.row0 + i;
     const int qh = head * p.group + g;
     const int see_hi = !real ? 0 : p.causal ? min(hi, q.pos0 + i + 1) : hi;
     const int see_lo = p.window ? max(lo, q.pos0 + i - p.window + 1) : lo;

@@ -58,8 +58,7 @@ struct AttnParams {
     FastDiv group_div, kv_div, heads_div;
     int short_limit;              // rows x group of a sequence up to which it goes in short tiles
     int short_shift;              // rows of a short tile, as a power of two
-    int short_blocks;             // workgroups that share the short tiles
-    int join_blocks, join_rows, join_long;   // ends of their stretches, workgroups for each, and workgroups that join long tiles' parts
+    int short_blocks, join_blocks;   // workgroups that share the short tiles, and that join their parts
     int32_t *plan;                // device: see kv_attention.h
     float *part_o, *part_ml;      // partial results of short tiles whose range is cut: sums, and maximum and sum of weights
     float *long_o, *long_ml;
@@ -69,6 +68,8 @@ struct AttnParams {
     float *whole_o, *whole_ml;    // of groups' rows and heads: over the shared tokens, then over their own
     int4 *found;                  // of the same: where their parts are (kv_attention.h)
     int parts_short, parts_long;  // partial results that there is room for
+    // (behind the others, whose places decide how the attention kernels' registers are loaded: in front of `plan` it cost one 5 %)
+    int join_long;                // workgroups that join long tiles' parts
 };
 
 struct ShareParams {
