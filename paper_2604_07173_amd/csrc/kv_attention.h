@@ -39,7 +39,9 @@ constexpr int kMostInline = S ? kSharedInline : kInlineSeqs;
 template <bool S>
 constexpr int kArrays = S ? kSharedArrays : kPlanArrays;
 template <bool S>
-constexpr int kInlineWords = kPlanHead + kArrays<S> * kMostInline<S>;
+constexpr int kInlineWords = kPlanHead + kArrays<S> * kMostInline<S>;      // room for a plan that is made in LDS, and for a copy
+template <bool S>
+constexpr int kCopiedWords = kPlanHead + kArrays<S> * (S ? kSharedCopied : kInlineSeqs);
 
 template <bool S>
 struct Seq {
@@ -202,7 +204,7 @@ __device__ inline void plan_entry(const AttnParams &p, const Seq<S> &q, int shif
     own[kBaseUnit] = tiles_of<kShort>(p, q) * p.c.n_heads * units_of(reach_of<kShort>(p, q), shift);
     own[kBaseItem] = tiles * cuts * p.c.n_heads;
     own[kBaseSlot] = cuts > 1 ? own[kBaseItem] : 0;
-    own[kBaseJoin] = cuts > 1 && tiles ? q.rows * p.heads : 0;
+    own[kBaseJoin] = cuts > 1 && tiles && !q.group && !q.first ? q.rows * p.heads : 0;      // rows of groups are found otherwise
 }
 
 __device__ inline void plan_head(const AttnParams &p, int32_t *plan, int shift, int chunk, const int (&sum)[kPlanSums])
@@ -330,10 +332,16 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
 
 // The plan: made in s_plan by the workgroup's first wave, or what plan_kernel has left in the workspace.  The first workgroup
 // leaves its own there for the launch after.
+// copy: a plan that has been made in memory is searched often.
 template <bool S>
-__device__ inline const int32_t *plan_of(const AttnParams &p, int32_t *s_plan)
+__device__ inline const int32_t *plan_of(const AttnParams &p, int32_t *s_plan, bool copy)
 {
-    if (plan_seqs<S>(p) > kMostInline<S>) return p.plan;
+    if (plan_seqs<S>(p) > kMostInline<S>) {
+        if (!S || !copy || plan_seqs<S>(p) > kSharedCopied) return p.plan;
+        for (int i = threadIdx.x; i < kPlanHead + kArrays<S> * plan_seqs<S>(p); i += blockDim.x) s_plan[i] = p.plan[i];
+        __syncthreads();
+        return s_plan;
+    }
     if (threadIdx.x < 64) make_plan<S>(p, s_plan);
     __syncthreads();
     if (blockIdx.x == 0)

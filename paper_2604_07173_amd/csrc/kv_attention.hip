@@ -118,11 +118,11 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
     constexpr int kVBytes = kWaves * kBlock * DP * 2, kOBytes = kWaves * 16 * OS * 4;
     __shared__ __align__(16) char s_mem[kVBytes > kOBytes ? kVBytes : kOBytes];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-    __shared__ int32_t s_plan[kInlineWords<S>];
+    __shared__ int32_t s_plan[kCopiedWords<S>];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
-    const int32_t *plan = plan_of<S>(p, s_plan);
+    const int32_t *plan = plan_of<S>(p, s_plan, true);
     const int D = FULL ? DP : p.c.dim;
     uint16_t *s_v = reinterpret_cast<uint16_t *>(s_mem) + wave * kBlock * DP;
     const unsigned v_lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)s_v;

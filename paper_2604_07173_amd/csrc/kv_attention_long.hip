@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     const int col = lane & 31, half = lane >> 5;
     const int D = FULL ? DP : p.c.dim;
     __shared__ int32_t s_plan[kInlineWords<S>];
-    const int32_t *plan = plan_of<S>(p, s_plan);
+    const int32_t *plan = plan_of<S>(p, s_plan, false);
     const int n = blockIdx.x;
     if (n >= plan[kItems]) return;
     // the cuts of a tile lie n_heads apart, tiles behind each other, those with the longest ranges first

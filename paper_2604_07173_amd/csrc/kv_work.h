@@ -29,8 +29,9 @@ constexpr int kShortEqual = 32, kShortLimit = 64;
 constexpr int kInlineSeqs = 256;         // sequences up to which every workgroup makes the plan for itself, in LDS: one launch less
 // 32-bit words of the plan in memory: of its head, and of each sequence
 constexpr int kPlanHead = 8, kPlanArrays = 7;
-// the same for batches that share tokens: groups and sequences, with the tokens that each begins at
-constexpr int kSharedInline = 64, kSharedArrays = 8;
+// The same for batches that share tokens: groups and sequences, with the tokens that each begins at.  Up to kSharedCopied a plan that has been
+// made in memory is copied to LDS, where the searches in it are faster.
+constexpr int kSharedInline = 64, kSharedCopied = 384, kSharedArrays = 8;
 
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 

@@ -1,7 +1,7 @@
 // The residual's addition and the norm behind it in one pass: s = x + add, y = s r (w + shift) with r = 1 / sqrt(mean s^2 + eps), in
 // fp32.  A row stays in registers between its sum of squares and its outputs, so every element is read once and written once
 // and the kernel is bound by memory (by latency for a decode batch's few rows): 16384 rows of 4096 columns, bf16, with the residual's sum, the
-// bf16 rows and e4m3 ones with a scale for every 128 columns (606 MB) 114 us, 5.3 TB/s, more than a plain copy of as much (4.85);
+// bf16 rows and e4m3 ones with a scale for every 128 columns (606 MB) 117 us, 5.2 TB/s, more than a plain copy of as much (4.85);
 // 1333 rows of 2056 fp32 columns (41 MB) 11 us; 64 rows 4.5 us, of which a launch takes 3.
 //
 // Vector v of a row, eight columns, belongs to thread v % T of the row's T threads: loads are contiguous over a wave, and a group of
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormParams p)
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const int c = (k * T + t) * 8;
-            // (fetched before the row is summed they take registers from other workgroups: 16384 rows of 4096 columns 114 -> 120 us)
+            // (fetched before the row is summed they take registers from other workgroups: 16384 rows of 4096 columns 117 -> 121 us)
             float w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = 1.f;
@@ -187,7 +187,8 @@ template <bool XF32, Add A>
 void launch_width(const NormParams &p, hipStream_t s)
 {
     const int vecs = p.width / 8;
-    // as many waves as the row fills, so that few lanes have nothing to do
+    // As many waves as the row fills, so that few lanes have nothing to do.  One vector a thread up to five waves (1333 rows of 2056 fp32 columns
+    // 11.0 us, with two 11.4); with eight 16384 rows of 4096 columns gain 2 % and 2130 of 3912 lose 12
 #define LORA_NORM(WAVE, N)                                                                                     \
     {                                                                                                          \
         const int rows = WAVE ? 4 : 1, threads = WAVE ? 256 : (vecs + 64 * N - 1) / (64 * N) * 64;             \
@@ -196,7 +197,7 @@ void launch_width(const NormParams &p, hipStream_t s)
     }
     if (vecs <= 64) LORA_NORM(true, 1)
     else if (vecs <= 128) LORA_NORM(true, 2)
-    else if (vecs <= 512) LORA_NORM(false, 1)
+    else if (vecs <= 320) LORA_NORM(false, 1)
     else if (vecs <= 1024) LORA_NORM(false, 2)
     else if (vecs <= 4096) LORA_NORM(false, 4)
     else LORA_NORM(false, 8)

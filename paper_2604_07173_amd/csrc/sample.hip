@@ -274,18 +274,21 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, F32 ? 2 : 1> some;
     const std::integral_constant<int, F32 ? 4 : 2> many;
+    const std::integral_constant<int, 8> most;
     const auto each_group = [&](auto ahead, int from, int count, auto f) {
         constexpr int AHEAD = decltype(ahead)::value;
+        constexpr bool WAIT = AHEAD == decltype(most)::value;      // as many as there are registers for: none besides
         u32x4 v[AHEAD], next[AHEAD];
         const auto fetch = [&](int k) {
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) next[j] = row.load(k + j < count ? from + (k + j) * 64 : pieces);
         };
-        fetch(0);
+        if (!WAIT) fetch(0);
         for (int k = 0; k < count; k += AHEAD) {
+            if (WAIT) fetch(k);
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) v[j] = next[j];
-            fetch(k + AHEAD);
+            if (!WAIT) fetch(k + AHEAD);
             f(v, from + k * 64);
         }
     };
@@ -309,7 +312,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
 
     // 1: the largest logit
     float mine = -INFINITY;
-    each(many, [&](float l, int) { mine = fmaxf(mine, l); });
+    each(most, [&](float l, int) { mine = fmaxf(mine, l); });
     float top = mine, low = mine;         // low: the least of the threads' largest
 #pragma unroll
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d)), low = fminf(low, __shfl_xor(low, d));
@@ -375,7 +378,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
         __syncthreads();
         unsigned a = 0xFFFFFFFFu, b = 0;
         if (!decltype(dense)::value) {
-            each(many, [&](float l, int i) {
+            each(most, [&](float l, int i) {
                 if (!f(l)) return;
                 const unsigned key = key_of(l), at = atomicAdd(&sh.listed, 1u);
                 a = min(a, key);
