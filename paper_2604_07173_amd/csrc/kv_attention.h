@@ -15,6 +15,8 @@
 // does not have.  Results of rows of groups stay partial, and whoever begins a tile says where its rows' parts are (`found`): of tiles
 // that are not cut in whole_o and whole_ml.  join_kernel puts them together.
 #pragma once
+#include <limits.h>
+
 #include "kv_device.h"
 #include "kv_work.h"
 
@@ -27,7 +29,7 @@ enum Kind { kShort, kLong };
 // The plan: a head of kPlanHead words, then kPlanArrays arrays over the sequences: units of short tiles before each
 // sequence, work items and partial results of long tiles, and rows x heads of long tiles to join; then the sequences
 // themselves.
-enum { kUnits, kShare, kUnitTokens, kChunk, kItems, kJoinUnits, kGroupRows, kHeadWords };
+enum { kUnits, kShare, kUnitTokens, kChunk, kItems, kJoinUnits, kGroupRows, kGroupLimit, kHeadWords };
 enum { kBaseUnit, kBaseItem, kBaseSlot, kBaseJoin, kPlanSums, kSeqRow0 = kPlanSums, kSeqRows, kSeqLen, kSeqArrays, kSeqFirst = kSeqArrays };
 static_assert(kHeadWords <= kPlanHead && kSeqArrays == kPlanArrays && kSeqFirst + 1 == kSharedArrays, "as many words as the host makes room for");
 
@@ -39,9 +41,7 @@ constexpr int kMostInline = S ? kSharedInline : kInlineSeqs;
 template <bool S>
 constexpr int kArrays = S ? kSharedArrays : kPlanArrays;
 template <bool S>
-constexpr int kInlineWords = kPlanHead + kArrays<S> * kMostInline<S>;      // room for a plan that is made in LDS, and for a copy
-template <bool S>
-constexpr int kCopiedWords = kPlanHead + kArrays<S> * (S ? kSharedCopied : kInlineSeqs);
+constexpr int kInlineWords = kPlanHead + kArrays<S> * kMostInline<S>;
 
 template <bool S>
 struct Seq {
@@ -125,12 +125,12 @@ __device__ inline void note(const AttnParams &p, int64_t row, int qh, int first,
     p.found[row * p.heads + qh] = int4{first, second, n, kind};
 }
 
-// Tiles that the sequence has of this kind.
+// Tiles that the sequence has of this kind.  group_limit: as short_limit, of a group's rows.
 template <Kind K, bool S>
-__device__ inline int tiles_of(const AttnParams &p, const Seq<S> &q)
+__device__ inline int tiles_of(const AttnParams &p, const Seq<S> &q, int group_limit)
 {
     const int n = q.rows * p.group;
-    if ((n <= (q.group ? p.group_limit : p.short_limit)) != (K == kShort)) return 0;
+    if ((n <= (q.group ? group_limit : p.short_limit)) != (K == kShort)) return 0;
     return K == kShort ? (n + (1 << p.short_shift) - 1) >> p.short_shift : (n + kLongTile - 1) / kLongTile;
 }
 
@@ -197,11 +197,11 @@ __device__ inline int cut_of(const Range &r, int splits)
 
 // What a sequence adds to the plan's arrays.
 template <bool S>
-__device__ inline void plan_entry(const AttnParams &p, const Seq<S> &q, int shift, int chunk, int (&own)[kPlanSums])
+__device__ inline void plan_entry(const AttnParams &p, const Seq<S> &q, int shift, int chunk, int group_limit, int (&own)[kPlanSums])
 {
-    const int tiles = tiles_of<kLong>(p, q);
+    const int tiles = tiles_of<kLong>(p, q, group_limit);
     const int cuts = splits_of(reach_of<kLong>(p, q), chunk);
-    own[kBaseUnit] = tiles_of<kShort>(p, q) * p.c.n_heads * units_of(reach_of<kShort>(p, q), shift);
+    own[kBaseUnit] = tiles_of<kShort>(p, q, group_limit) * p.c.n_heads * units_of(reach_of<kShort>(p, q), shift);
     own[kBaseItem] = tiles * cuts * p.c.n_heads;
     own[kBaseSlot] = cuts > 1 ? own[kBaseItem] : 0;
     own[kBaseJoin] = cuts > 1 && tiles && !q.group && !q.first ? q.rows * p.heads : 0;      // rows of groups are found otherwise
@@ -265,11 +265,17 @@ __device__ inline unsigned plan_faults_of(const AttnParams &p, int s)
     return s < p.g.most ? 0u : faults_of(p.b, s - p.g.most);
 }
 
-// The plan of up to kMostInline sequences, by one wave: lane l takes the sequences l * each .. of the batch.
-template <bool S>
+// S: what a group in long tiles adds to the work that decides whether there are any.
+__device__ inline float group_work(const AttnParams &p, const Seq<true> &q)
+{
+    const int n = q.rows * p.group;
+    return q.group && n > p.group_limit ? (float)n * (float)q.len * (float)p.c.n_heads : 0.f;
+}
+
+// The plan of up to 64 * MOST sequences, by one wave: lane l takes the sequences l * each .. of the batch.
+template <bool S, int MOST>
 __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
 {
-    constexpr int MOST = kMostInline<S> / 64;
     const int lane = threadIdx.x & 63, n = plan_seqs<S>(p), each = (n + 63) >> 6;
     Seq<S> q[MOST];
     unsigned bad = 0;
@@ -283,18 +289,25 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
             bad |= plan_faults_of<S>(p, s);
         }
     }
+    int group_limit = p.group_limit;
+    if constexpr (S) {
+        float all = 0.f;
+#pragma unroll
+        for (int k = 0; k < MOST; ++k) all += group_work(p, q[k]);
+        if (last_lane(wave_scan(all)) <= kGroupsShort) group_limit = INT_MAX;
+    }
     float units = 0.f;
 #pragma unroll
-    for (int k = 0; k < MOST; ++k) units += (float)(tiles_of<kShort>(p, q[k]) * p.c.n_heads) * (float)units_of(reach_of<kShort>(p, q[k]), kUnitShift);
+    for (int k = 0; k < MOST; ++k) units += (float)(tiles_of<kShort>(p, q[k], group_limit) * p.c.n_heads) * (float)units_of(reach_of<kShort>(p, q[k]), kUnitShift);
     const int shift = unit_shift_of(last_lane(wave_scan(units)));
     int chunk = 1 << 30;
     if (p.long_o) {
 #pragma unroll
-        for (int k = 0; k < MOST; ++k) work += (float)tiles_of<kLong>(p, q[k]) * (float)reach_of<kLong>(p, q[k]);
+        for (int k = 0; k < MOST; ++k) work += (float)tiles_of<kLong>(p, q[k], group_limit) * (float)reach_of<kLong>(p, q[k]);
         float tiles = 0.f;
         if (S) {
 #pragma unroll
-            for (int k = 0; k < MOST; ++k) tiles += (float)tiles_of<kLong>(p, q[k]);
+            for (int k = 0; k < MOST; ++k) tiles += (float)tiles_of<kLong>(p, q[k], group_limit);
             tiles = last_lane(wave_scan(tiles));
         }
         chunk = chunk_of<S>(p, last_lane(wave_scan(work)), tiles);
@@ -305,7 +318,7 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
 #pragma unroll
         for (int k = 0; k < MOST; ++k) {
             if (k >= each) break;
-            plan_entry(p, q[k], shift, chunk, own[k]);
+            plan_entry(p, q[k], shift, chunk, group_limit, own[k]);
 #pragma unroll
             for (int a = 0; a < kPlanSums; ++a) sum[a] += own[k][a];
         }
@@ -326,23 +339,20 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
     for (int k = 0; k < MOST; ++k)
         if (k < each && lane * each + k < n) store_seq<S>(plan, n, lane * each + k, q[k]);
     if (lane == 63) plan_head(p, plan, shift, chunk, sum);
-    if (S && lane == 63) plan[kGroupRows] = group_rows(p, no_rows);
+    if (S && lane == 63) plan[kGroupRows] = group_rows(p, no_rows), plan[kGroupLimit] = group_limit;
     if (bad && blockIdx.x == 0) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
 }
 
 // The plan: made in s_plan by the workgroup's first wave, or what plan_kernel has left in the workspace.  The first workgroup
 // leaves its own there for the launch after.
-// copy: a plan that has been made in memory is searched often.
 template <bool S>
-__device__ inline const int32_t *plan_of(const AttnParams &p, int32_t *s_plan, bool copy)
+__device__ inline const int32_t *plan_of(const AttnParams &p, int32_t *s_plan)
 {
-    if (plan_seqs<S>(p) > kMostInline<S>) {
-        if (!S || !copy || plan_seqs<S>(p) > kSharedCopied) return p.plan;
-        for (int i = threadIdx.x; i < kPlanHead + kArrays<S> * plan_seqs<S>(p); i += blockDim.x) s_plan[i] = p.plan[i];
-        __syncthreads();
-        return s_plan;
+    if (plan_seqs<S>(p) > kMostInline<S>) return p.plan;
+    if (threadIdx.x < 64) {
+        if (S && plan_seqs<S>(p) <= 64) make_plan<S, 1>(p, s_plan);
+        else make_plan<S, kMostInline<S> / 64>(p, s_plan);
     }
-    if (threadIdx.x < 64) make_plan<S>(p, s_plan);
     __syncthreads();
     if (blockIdx.x == 0)
         for (int i = threadIdx.x; i < kPlanHead + kArrays<S> * plan_seqs<S>(p); i += blockDim.x) p.plan[i] = s_plan[i];

@@ -41,12 +41,24 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = plan_seqs<S>(p);
     float work = 0.f, units = 0.f, tiles = 0.f;
     unsigned bad = 0;
+    int group_limit = p.group_limit;
+    if constexpr (S) {
+        float all = 0.f;
+        for (int s = tid; s < p.g.most; s += kPlanThreads) all += group_work(p, seq_of<true>(p, s));
+        all = wave_scan(all);
+        if (lane == 63) s_work[wave] = all;
+        __syncthreads();
+        all = 0.f;
+        for (int w = 0; w < WAVES; ++w) all += s_work[w];
+        __syncthreads();                  // s_work is used again
+        if (all <= kGroupsShort) group_limit = INT_MAX;
+    }
     for (int s = tid; s < n; s += kPlanThreads) {
         const Seq<S> q = seq_of<S>(p, s);
         bad |= plan_faults_of<S>(p, s);
-        work += (float)tiles_of<kLong>(p, q) * (float)reach_of<kLong>(p, q);
-        if (S) tiles += (float)tiles_of<kLong>(p, q);
-        units += (float)(tiles_of<kShort>(p, q) * p.c.n_heads) * (float)units_of(reach_of<kShort>(p, q), kUnitShift);
+        work += (float)tiles_of<kLong>(p, q, group_limit) * (float)reach_of<kLong>(p, q);
+        if (S) tiles += (float)tiles_of<kLong>(p, q, group_limit);
+        units += (float)(tiles_of<kShort>(p, q, group_limit) * p.c.n_heads) * (float)units_of(reach_of<kShort>(p, q), kUnitShift);
     }
     if (bad) atomicOr(p.b.status, LORA_STATUS_BAD_LENGTH);
     work = wave_scan(work);
@@ -64,7 +76,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
         int own[kPlanSums] = {}, upto[kPlanSums];
         if (s < n) {
             const Seq<S> q = seq_of<S>(p, s);
-            if (!no_rows) plan_entry(p, q, shift, chunk, own);
+            if (!no_rows) plan_entry(p, q, shift, chunk, group_limit, own);
             store_seq<S>(p.plan, n, s, q);
         }
         __syncthreads();                  // the round before has been read
@@ -86,7 +98,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
         }
     }
     if (tid == 0) plan_head(p, p.plan, shift, chunk, base);
-    if (S && tid == 0) p.plan[kGroupRows] = group_rows(p, no_rows);
+    if (S && tid == 0) p.plan[kGroupRows] = group_rows(p, no_rows), p.plan[kGroupLimit] = group_limit;
 }
 
 // V^T of 16 columns and a block's 32 tokens, in the order of the second product (see above).
@@ -118,11 +130,11 @@ __global__ __launch_bounds__(kWaves * 64, BLOCKS) void attend_kernel(AttnParams 
     constexpr int kVBytes = kWaves * kBlock * DP * 2, kOBytes = kWaves * 16 * OS * 4;
     __shared__ __align__(16) char s_mem[kVBytes > kOBytes ? kVBytes : kOBytes];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-    __shared__ int32_t s_plan[kCopiedWords<S>];
+    __shared__ int32_t s_plan[kInlineWords<S>];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
-    const int32_t *plan = plan_of<S>(p, s_plan, true);
+    const int32_t *plan = plan_of<S>(p, s_plan);
     const int D = FULL ? DP : p.c.dim;
     uint16_t *s_v = reinterpret_cast<uint16_t *>(s_mem) + wave * kBlock * DP;
     const unsigned v_lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)s_v;
@@ -550,10 +562,9 @@ void lay_out(AttnParams &p, const Kinds &k, const AttnWs &at, void *ws)
     p.short_blocks = k.blocks;
 }
 
-// The kernels of short tiles and the join.  tiles: short tiles of a head, at most; join_rows: rows of a tile that join_kernel
-// takes side by side; shared: workgroups for the rows of groups.
+// The kernel of short tiles, `tiles` of a head at most; its workgroups.
 template <bool S>
-hipError_t launch_short_and_join(AttnParams &p, const Kinds &k, int64_t reach, int64_t tiles, unsigned join_rows, unsigned shared, hipStream_t s)
+unsigned launch_short(const AttnParams &p, const Kinds &k, int64_t reach, int64_t tiles, hipStream_t s)
 {
     unsigned grid = 0;
     if (k.has_short) {
@@ -564,6 +575,14 @@ hipError_t launch_short_and_join(AttnParams &p, const Kinds &k, int64_t reach, i
         else if (p.c.dim <= 128) launch_attend<128, 1, 3, S>(p, grid, s);
         else launch_attend<256, 1, 2, S>(p, grid, s);
     }
+    return grid;
+}
+
+// The join of the short tiles' parts that `grid` workgroups have left, and of the long tiles'.  join_rows: rows of a tile that
+// join_kernel takes side by side; shared: workgroups for the rows of groups.
+template <bool S>
+hipError_t launch_join(AttnParams &p, const Kinds &k, int64_t reach, unsigned grid, unsigned join_rows, unsigned shared, hipStream_t s)
+{
     // parts: of short tiles of more than one unit, of long ones that may be cut
     p.join_long = k.has_long && reach > kLongMinSplit ? 1024 : 0;
     p.join_blocks = k.has_short && reach > 1 << kUnitShift ? (int)grid - 1 : 0;
@@ -612,7 +631,7 @@ hipError_t launch_attention(AttnParams &p, int max_rows, void *ws, hipStream_t s
     const int64_t tiles = std::min(p.b.n_seqs, p.b.n_rows) + ((int64_t)p.b.n_rows * p.group >> k.shift);
     // a wave per row of a tile, or per four rows where most sequences are likely to have one new row only
     const unsigned rows = k.has_long ? 1 : (unsigned)std::min<int64_t>(1 << k.shift, (int64_t)(max_rows > 0 ? max_rows : p.b.n_rows) * p.group);
-    return launch_short_and_join<false>(p, k, reach, tiles, rows, 0, s);
+    return launch_join<false>(p, k, reach, launch_short<false>(p, k, reach, tiles, s), rows, 0, s);
 }
 
 size_t attention_shared_ws_bytes(int n_seqs, int n_rows, int max_rows, int group_rows, int max_group_rows, int heads, int kv_heads, int dim)
@@ -633,15 +652,17 @@ hipError_t launch_attention_shared(AttnParams &p, int max_rows, int max_group_ro
     p.parts_short = 2 * k.blocks << k.shift;
     p.parts_long = k.has_long ? 2 * kSharedTarget * kLongTile : 0;
     if (p.g.most + p.b.n_seqs > kSharedInline) hipLaunchKernelGGL(plan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, s, p);
+    const int64_t rows = (int64_t)p.b.n_rows + p.g.most_rows;
+    const int64_t tiles = std::min(p.b.n_seqs, p.b.n_rows) + p.g.most + (rows * p.group >> k.shift);
+    const unsigned shared = (unsigned)std::min<int64_t>(((int64_t)p.g.most_rows * p.heads + 3) / 4, 8192);
+    // the short tiles' kernel first: it leaves a plan that it has made to the long ones', which so has little to do where there are none
+    const unsigned grid = launch_short<true>(p, k, p.b.tokens_max, tiles, s);
     if (k.has_long) {
         const hipError_t e = launch_attend_long_shared(p, (int)k.long_items, s);
         if (e != hipSuccess) return e;
     }
-    const int64_t rows = (int64_t)p.b.n_rows + p.g.most_rows;
-    const int64_t tiles = std::min(p.b.n_seqs, p.b.n_rows) + p.g.most + (rows * p.group >> k.shift);
-    const unsigned shared = (unsigned)std::min<int64_t>(((int64_t)p.g.most_rows * p.heads + 3) / 4, 8192);
     // most tiles are of groups or of sequences in one, and the workgroups behind join them
-    return launch_short_and_join<true>(p, k, p.b.tokens_max, tiles, 4, shared, s);
+    return launch_join<true>(p, k, p.b.tokens_max, grid, 4, shared, s);
 }
 
 }  // namespace lora

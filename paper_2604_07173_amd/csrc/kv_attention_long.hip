@@ -79,8 +79,9 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int D = FULL ? DP : p.c.dim;
-    __shared__ int32_t s_plan[kInlineWords<S>];
-    const int32_t *plan = plan_of<S>(p, s_plan, false);
+    __shared__ int32_t s_plan[S ? 1 : kInlineWords<S>];
+    // (S: the kernels before have left it)
+    const int32_t *plan = S ? p.plan : plan_of<S>(p, s_plan);
     const int n = blockIdx.x;
     if (n >= plan[kItems]) return;
     // the cuts of a tile lie n_heads apart, tiles behind each other, those with the longest ranges first
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 ? 1 : 2) void attend_long_ker
     const int chunk = uniform(plan[kChunk]);
     const int cuts = splits_of(reach_of<kLong>(p, q), chunk);
     const int turn_no = cuts == 1 ? pair : pair / cuts, cut = pair - turn_no * cuts;
-    const int tile = tiles_of<kLong>(p, q) - 1 - turn_no;
+    const int tile = tiles_of<kLong>(p, q, S ? uniform(plan[kGroupLimit]) : 0) - 1 - turn_no;
     const Range rg = range_of<kLong>(p, q, tile);
     const int splits = splits_of(rg.hi - rg.lo, chunk);
     if (cut >= splits) return;

@@ -29,9 +29,9 @@ constexpr int kShortEqual = 32, kShortLimit = 64;
 constexpr int kInlineSeqs = 256;         // sequences up to which every workgroup makes the plan for itself, in LDS: one launch less
 // 32-bit words of the plan in memory: of its head, and of each sequence
 constexpr int kPlanHead = 8, kPlanArrays = 7;
-// The same for batches that share tokens: groups and sequences, with the tokens that each begins at.  Up to kSharedCopied a plan that has been
-// made in memory is copied to LDS, where the searches in it are faster.
-constexpr int kSharedInline = 64, kSharedCopied = 384, kSharedArrays = 8;
+// The same for batches that share tokens: groups and sequences, with the tokens that each begins at (256 sequences in 16 groups: 124 us; with the
+// plan made in a launch of its own and searched in memory 152; of 64 and fewer a lane takes one each: 8 sequences 14.9 us, otherwise 15.7)
+constexpr int kSharedInline = kInlineSeqs + kInlineSeqs / 2, kSharedArrays = 8;
 
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -79,7 +79,12 @@ struct SharedKinds : Kinds {
 };
 
 constexpr int64_t kSharedRowsHeads = 1 << 26;      // rows x heads of such a batch: its long tiles, of 17 rows or more, make no grid too large
-constexpr int kGroupShort = 32;          // rows x group up to which a group goes in short tiles
+// Groups of more rows x group than kGroupShort go in long tiles, unless all their rows x group x shared tokens x key/value heads together are
+// no more than kGroupsShort: short tiles then fill the chip as well, and it is their latency that counts (32 / 8 heads of 128: 32 answers over
+// 1000 tokens 21.7 us, in long tiles 33.5; two groups of 32 over 1000 33.7 and 42.1, two of 64 over 700 49.0 and 49.3; 16 of 16 over 1000 to 6000 157 and
+// 124).  Eight answers over 1500 tokens, 32 rows x group, take 14 us and in long tiles 35.
+constexpr int kGroupShort = 32;
+constexpr float kGroupsShort = 2.8e6f;
 // Items of long tiles that fill the chip where tokens are shared: two on every CU, as long as they are no shorter than kLongMinSplit
 constexpr int kSharedTarget = 512;
 
