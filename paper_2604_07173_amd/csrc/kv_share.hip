@@ -21,8 +21,9 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kSeqsInLds = 1024;          // sequences whose arrays fit in LDS
 constexpr int kWide = 4;                  // entries of a table that a lane compares at a time
-// Rounds of comparing that the waves of one workgroup take on, at most: sequences x their rounds.
-constexpr int kOneLaunch = 8 * kWaves;
+// Rounds of comparing that the waves of one workgroup take on, at most: sequences x their rounds (of one round each, in one launch and in
+// three: 4 sequences 7.8 and 12.5 us, 32 10.3 and 13.1, 64 11.5 and 13.4, 128 16.9 and 13.8, 256 28.3 and 14.8).
+constexpr int kOneLaunch = 5 * kWaves;
 
 typedef unsigned long long u64;
 

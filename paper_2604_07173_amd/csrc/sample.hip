@@ -16,7 +16,10 @@
 // cubic term (below 2^-37) is put into the linear one, which leaves a quarter of it; and taken as a whole multiple of 2^-shift: the sums
 // of whole numbers are exact, so threads may add them in any order.  The order of tokens is that of the logits' bits.
 //
-// Bound by the instructions that form weights, 24 for each token that has one, at four cycles a wave; the reading of the row comes second.
+// Bound by the instructions that form weights, 24 for each token that has one, four cycles a wave at 64 bits (28 us for 128000 tokens of a
+// row), and by the latency of a pass and of its sums over the workgroup, some 3 us each; the reading comes third.  64 rows of
+// 128000 fp32 logits (33 MB) with limits of their own 100 us, 512 of 50257 bf16 (51 MB) with top_p = 0.95 68 us, one of 32000 with top_k = 50 and
+// top_p = 0.9 12.5 us, of which a launch takes 3.
 #include <limits.h>
 
 #include <algorithm>
@@ -32,8 +35,16 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int kTable = 1024;
-// Rows up to which each has a CU to itself, whose waves all work on it.
-constexpr int kRowsAlone = 256;
+// Rows up to which each has a CU to itself, whose waves all work on it; more share CUs, in workgroups of half as many.  Small vocabularies
+// take fewer threads, so that barriers and sums over the workgroup cost less.  us, T = 1 and top_p = 0.95 unless said, 1024 / 512 / 256 threads:
+//   256 rows of 64000 fp32     60.5 /  61.7 /  99      512 rows of 128000 bf16   153.9 / 136.4
+//   64 of 200000              106.7 / 141.6            1024 of 64000             185.0 / 143.6
+//   1 of 32000                 30.9 /  32.5 /  47      512 of 50257, top_k 50     35.0 /  27.2
+// and with limits that differ from row to row (300 rows of which few take long: 72 / 109, 1024 rows: 172 / 148)
+//   64 of 16000                39.8 /  38.4 /  51.5    1 of 4000                  25.8 /  17.2 /  17.6
+//   64 of 8192                 35.4 /  29.3 /  34.2    64 of 1000                   -  /  22.0 /  20.2
+//   1024 of 8000                 -  /  50.1 /  42.5    1024 of 32000             122.5 /  88.2 /  93.2
+constexpr int kRowsAlone = 256, kSmallVocab = 16384, kTinyVocab = 2048, kTinyVocabMany = 8192;
 constexpr double kMagic = 4503599627370496.0;      // 2^52: added to a number below it, leaves its rounding to a whole one in the low bits
 
 // The order of floats as that of whole numbers; -0 and 0 are one value.
@@ -193,8 +204,11 @@ struct Shared {
     static constexpr int BINS = 256;                     // of falling logits, over 32 powers of two of weights, for every wave
     static constexpr int COUNTS = 4 * THREADS;           // the same over 48, beyond which no token has a weight
     static constexpr int FINE = THREADS;                 // of the values' bits
-    static constexpr int LISTED = 4 * THREADS;           // tokens of a list
-    static constexpr int FEW = THREADS / 2;              // tokens of a list that are compared in pairs
+    // tokens of a list: as many as LDS holds, for bins with more are read from the row again, three times (64 rows of 200000 273 us with
+    // a list of 4096, now 162)
+    static constexpr int LISTED = THREADS == 1024 ? 14336 : THREADS == 512 ? 6144 : 1024;
+    // tokens of a list that are compared in pairs (400 of 512 tokens 64 us, in bins 28)
+    static constexpr int FEW = THREADS > 256 ? 256 : 128;
     double table[kTable];
     union {
         u64 mass[WAVES][BINS];
@@ -313,7 +327,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
     // 1: the largest logit
     float mine = -INFINITY;
     each(most, [&](float l, int) { mine = fmaxf(mine, l); });
-    float top = mine, low = mine;         // low: the least of the threads' largest
+    float top = mine, low = mine > -INFINITY ? mine : INFINITY;          // low: the least of the threads' largest
 #pragma unroll
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d)), low = fminf(low, __shfl_xor(low, d));
     if (lane == 0) sh.wave_top[wave] = top, sh.wave_low[wave] = low;
@@ -463,18 +477,20 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
     // 2: the first k of the order
     if (by_k) {
         const u64 want = (u64)k_most;
-        const float per = (float)FINE / (top - low);
-        if (k_most <= THREADS / 4 * 3 && low > -INFINITY && low < top && per < 1e30f) {
+        float per = low < top ? (float)FINE / (top - low) : 1.f;
+        if (k_most <= THREADS / 4 * 3 && per > 0.f && per < 1e30f) {
             // bins of the threads' largest, from the row's down to the least of them
             sh.fine.count[tid] = 0;
             __syncthreads();
-            atomicAdd(&sh.fine.count[(int)fminf((top - mine) * per, (float)(FINE - 1))], 1u);
+            if (mine > -INFINITY) atomicAdd(&sh.fine.count[(int)fminf((top - mine) * per, (float)(FINE - 1))], 1u);
             __syncthreads();
             find_bin<THREADS, 1>(sh, {sh.fine.count[tid]}, want);
-            // tokens of that bin and of those before it: by the same function, so that none of the k is missed
-            const float end = sh.bin == FINE - 1 ? INFINITY : (float)(sh.bin + 1);
+            // tokens of that bin and of those before it: by the same function, so that none of the k is missed.  All, where fewer
+            // than k threads have any, if no difference is too large
+            if (sh.bin < 0) per = 0x1p-100f;
+            const float end = sh.bin < 0 || sh.bin == FINE - 1 ? INFINITY : (float)(sh.bin + 1);
             listed = list(no, [&](float l) { return (top - l) * per < end; }, lo, hi);
-            in_list = listed <= Lds::LISTED;
+            in_list = listed <= Lds::LISTED && (sh.bin >= 0 || top < 0x1p102f);
         }
         if (in_list && listed <= Lds::FEW) {
             // `side` neighbouring threads per token, each for every side-th of the others
@@ -520,7 +536,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
         }
         const auto all = [](float) { return true; };
         if (in_list) {
-            border = refine(no, all, lo, hi, listed, want, 0);
+            if (listed >= want) border = refine(no, all, lo, hi, listed, want, 0);
         } else {
             for (int i = tid; i < COUNTS; i += THREADS) sh.count[i] = 0;
             __syncthreads();
@@ -737,8 +753,8 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
 template <bool F32>
 void launch(const SampleParams &p, hipStream_t s)
 {
-    if (p.vocab <= 8192) hipLaunchKernelGGL((sample_kernel<F32, 256>), dim3(p.n_rows), dim3(256), 0, s, p);
-    else if (p.n_rows > kRowsAlone) hipLaunchKernelGGL((sample_kernel<F32, 512>), dim3(p.n_rows), dim3(512), 0, s, p);
+    if (p.vocab <= (p.n_rows > kRowsAlone ? kTinyVocabMany : kTinyVocab)) hipLaunchKernelGGL((sample_kernel<F32, 256>), dim3(p.n_rows), dim3(256), 0, s, p);
+    else if (p.n_rows > kRowsAlone || p.vocab <= kSmallVocab) hipLaunchKernelGGL((sample_kernel<F32, 512>), dim3(p.n_rows), dim3(512), 0, s, p);
     else hipLaunchKernelGGL((sample_kernel<F32, 1024>), dim3(p.n_rows), dim3(1024), 0, s, p);
 }
 

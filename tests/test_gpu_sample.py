@@ -119,6 +119,37 @@ def test_lists_of_all_lengths(V, k, kind):
     check(x, u=us(6), k=k, p=0.8)
 
 
+@pytest.mark.parametrize("V,R", [(1500, 6), (12000, 6), (12000, 260), (50257, 4), (200001, 4)])
+@pytest.mark.parametrize("left", [1, 2, 40, 129, 300, 700, 5000, 20000])
+def test_rows_of_which_a_mask_leaves_few(V, R, left):
+    """Fewer tokens than top_k, than the workgroup has threads, than a list takes, in a stretch of the row and anywhere in it."""
+    g = torch.Generator().manual_seed(left)
+    left = min(left, V)
+    for near in (False, True):
+        x = torch.full((R, V), -math.inf)
+        for r in range(R):
+            at = torch.randperm(V, generator=g)[:left] if not near else (torch.arange(left) + int(torch.randint(0, V, (1,), generator=g))) % V
+            x[r, at] = 2.5 * torch.randn(left, generator=g)
+        x = x[:6].cuda() if R <= 6 else x.cuda()
+        rows = np.arange(R) % 4
+        check(x, k=np.array([1, 50, 400, 760])[rows], u=us(R))
+        check(x, k=np.array([50, 400, 760, 3000])[rows], p=0.9, u=us(R, 1), T=1.3)
+        if R > 6:
+            return
+
+
+def test_logits_as_far_apart_as_floats_are():
+    """Differences that are infinite in 32 bits."""
+    x = torch.full((4, 3000), -math.inf)
+    x[:, 1234] = 3e38
+    x[:, 77] = -3e38
+    x[2:, 78] = 1e38
+    x = x.cuda()
+    for k in (1, 2, 3, 50):
+        check(x, T=2e38, k=k, u=us(4, k))
+        check(x, T=2e38, k=k, p=0.97, u=us(4, k))
+
+
 def test_all_of_u():
     """One row's tokens over a fine grid of u, the ends among it."""
     R = 500
