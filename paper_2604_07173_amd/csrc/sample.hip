@@ -36,15 +36,16 @@ typedef unsigned long long u64;
 
 constexpr int kTable = 1024;
 // Rows up to which each has a CU to itself, whose waves all work on it; more share CUs, in workgroups of half as many.  Small vocabularies
-// take fewer threads, so that barriers and sums over the workgroup cost less.  us, T = 1 and top_p = 0.95 unless said, 1024 / 512 / 256 threads:
-//   256 rows of 64000 fp32     60.5 /  61.7 /  99      512 rows of 128000 bf16   153.9 / 136.4
-//   64 of 200000              106.7 / 141.6            1024 of 64000             185.0 / 143.6
-//   1 of 32000                 30.9 /  32.5 /  47      512 of 50257, top_k 50     35.0 /  27.2
-// and with limits that differ from row to row (300 rows of which few take long: 72 / 109, 1024 rows: 172 / 148)
-//   64 of 16000                39.8 /  38.4 /  51.5    1 of 4000                  25.8 /  17.2 /  17.6
-//   64 of 8192                 35.4 /  29.3 /  34.2    64 of 1000                   -  /  22.0 /  20.2
-//   1024 of 8000                 -  /  50.1 /  42.5    1024 of 32000             122.5 /  88.2 /  93.2
+// take fewer threads, so that barriers and sums over the workgroup cost less.  us with top_p = 0.95, 1024 / 512 / 256 threads:
+//   256 rows of 64000 fp32     60.1 /  62.1 /  99      512 rows of 128000 bf16   154.2 / 135.6 / 501
+//   64 of 200000              107.3 / 142.0 / 854      1024 of 64000             186.0 / 141.9 / 147
+//   1 of 32000                 30.6 /  32.3 /  47      64 of 2000                 21.1 /  16.8 /  15.7
+// and with limits that differ from row to row (300 rows of 64000, few of which take long: 64 / 78)
+//   64 of 16000                39.7 /  38.8 /  52      1 of 4000                  25.6 /  17.1 /  17.7
+//   64 of 8192                 35.2 /  29.0 /  34.8    64 of 1000                 28.6 /  22.0 /  20.3
+//   1024 of 8000               90.7 /  49.9 /  43.0    1024 of 32000             122.2 /  81.4 /  90.6
 constexpr int kRowsAlone = 256, kSmallVocab = 16384, kTinyVocab = 2048, kTinyVocabMany = 8192;
+// Of a row's tokens, the part at most that is listed whole
 constexpr int kListedOf = 4;
 constexpr double kMagic = 4503599627370496.0;      // 2^52: added to a number below it, leaves its rounding to a whole one in the low bits
 
