@@ -174,3 +174,22 @@ def test_on_another_stream():
     L.lora_kv_attention_shared(case.cache, 0, case.batch, sh, case.qd, 512, 8, out, 512, None, 0.125, ws, stream=side)
     side.synchronize()
     assert torch.equal(out, want[0])
+
+
+def test_two_calls_at_once_on_two_streams():
+    """Each with a workspace and results of its own; both kinds of tiles, cut ones among them."""
+    cases = [random_case(43, 60, 2, most=3, prompt_hi=2500, own_hi=60, heads=8, kv=2, dim=64).device(),
+             SharedCase([0] * 50, [3000], [7] * 50, [1] * 50, heads=32, kv=8, dim=128, seed=3).device()]
+    shares = [share(c) for c in cases]
+    want = [attend_shared(c, sh, 0.125)[0] for c, sh in zip(cases, shares)]
+    outs = [torch.zeros_like(w) for w in want]
+    wss = [torch.empty(L.lora_kv_attention_shared_ws_bytes(c.cache, c.batch, sh, c.heads), dtype=torch.uint8, device="cuda") for c, sh in zip(cases, shares)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c, sh, out, ws, st in zip(cases, shares, outs, wss, streams):
+            L.lora_kv_share(c.cache, c.batch, sh, stream=st)
+            L.lora_kv_attention_shared(c.cache, 0, c.batch, sh, c.qd, c.qd.stride(0), c.heads, out, out.shape[1], None, 0.125, ws, stream=st)
+    torch.cuda.synchronize()
+    for out, w in zip(outs, want):
+        assert torch.equal(out, w)

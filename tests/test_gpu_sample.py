@@ -249,3 +249,27 @@ def test_repeats_streams_and_graphs():
     L.lora_sample(x, V, R, V, how, ud, token, prob, stream=side)
     side.synchronize()
     assert torch.equal(token, call(x, T=0.9, k=500, p=0.9, u=us(R, 2))[0])
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+def test_many_rows_of_a_large_vocabulary(kind):
+    """Rows that share CUs: lists of a quarter of the row and more, whole or of one bin."""
+    R, V = 300, 20011
+    rng = np.random.default_rng(8)
+    check(logits(R, V, kind), T=rng.choice([0.0, 0.5, 1.0, 3.0], R), k=rng.choice([0, 40, 380, 400, 2000, 4900, 5100, 15000], R),
+          p=rng.choice([0.5, 0.95, 1.0], R), least=rng.choice([0.0, 0.0, 0.01], R), u=us(R, 3))
+
+
+def test_two_calls_at_once_on_two_streams():
+    xs = [logits(70, 40000), logits(300, 9000, torch.bfloat16)]
+    want = [call(x, T=0.8, k=3000, p=0.9, u=us(x.shape[0], 5)) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for x, st in zip(xs, streams):
+            with torch.cuda.stream(st):              # what the call is given is written on its stream
+                got.append(call(x, T=0.8, k=3000, p=0.9, u=us(x.shape[0], 5), stream=st))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
