@@ -404,17 +404,16 @@ struct RowSum {
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 };
 
-// Adds a row's parts: maxima and sums at ml[part(c) * 2], outputs at
-// po[part(c) * dim], for the parts c < n.  Lanes look at 64 parts' maxima and sums at a time, and hand their factors on to the
+// Adds a row's parts c < n: maximum and sum at ml(c), output at po(c).  Lanes look at 64 parts' maxima and sums at a time, and hand their factors on to the
 // lanes that add up the outputs: DP / 4 lanes take one part's 16 bytes each, eight sets of parts are on their way at once.
-template <int DP, class Part>
-__device__ inline void join_add(const AttnParams &p, RowSum &x, const float *ml, const float *po, int n, Part part)
+template <int DP, class Ml, class Out>
+__device__ inline void join_add(const AttnParams &p, RowSum &x, int n, Ml ml, Out po)
 {
     constexpr int LANES = DP / 4, SETS = 64 / LANES, DEEP = 8;
     const int lane = threadIdx.x & 63, set = lane / LANES, d = (lane % LANES) * 4, D = p.c.dim;
     for (int c0 = 0; c0 < n; c0 += 64) {
         const bool have = c0 + lane < n;
-        const float *at = ml + part(min(c0 + lane, n - 1)) * 2;
+        const float *at = ml(min(c0 + lane, n - 1));
         const float own_m = have ? at[0] : -INFINITY, own_l = have ? at[1] : 0.f;
         float now = own_m;
 #pragma unroll
@@ -433,7 +432,7 @@ __device__ inline void join_add(const AttnParams &p, RowSum &x, const float *ml,
             for (int k = 0; k < DEEP; ++k) {
                 const int cc = c + k * SETS + set;
                 o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (cc < some && d < D) o[k] = ld16f(po + part(c0 + cc) * D + d);
+                if (cc < some && d < D) o[k] = ld16f(po(c0 + cc) + d);
             }
 #pragma unroll
             for (int k = 0; k < DEEP; ++k) x.sum += o[k] * __shfl(f, min(c + k * SETS + set, 63));
@@ -470,17 +469,27 @@ __device__ inline int64_t short_part(const AttnParams &p, int b, int c, int star
     return (((int64_t)2 * (b + c) + (c == 0 && start != b * share)) << p.short_shift) + row;
 }
 
-// Adds what a row of a group and a head has come to.  Numbers that groups which are not true have left are kept in bounds.
-template <int DP>
-__device__ inline void join_found(const AttnParams &p, RowSum &x, int4 f)
-{
-    const bool is_short = f.w == kFoundShort, is_long = f.w == kFoundLong;
-    const float *ml = is_short ? p.part_ml : is_long ? p.long_ml : p.whole_ml, *o = is_short ? p.part_o : is_long ? p.long_o : p.whole_o;
-    const unsigned room = is_short ? p.parts_short : is_long ? p.parts_long : 2 * p.g.most_rows * p.heads;
-    const int by = is_short ? 2 << p.short_shift : p.c.n_heads * kLongTile, n = is_short || is_long ? min(max(f.z, 1), 4096) : 1;
-    if (!room) return;
-    join_add<DP>(p, x, ml, o, n, [&](int c) { return (int64_t)min((unsigned)(c == 0 ? f.x : f.y + (c - 1) * by), room - 1u); });
-}
+// Where the parts of a row of a group and a head are, over the shared tokens or over its own.  Numbers that groups which are not
+// true have left are kept in bounds.
+struct Found {
+    const float *ml, *o;
+    int first, second, n, by;
+    unsigned room;
+
+    __device__ Found(const AttnParams &p, int4 f)
+    {
+        const bool is_short = f.w == kFoundShort, is_long = f.w == kFoundLong;
+        ml = is_short ? p.part_ml : is_long ? p.long_ml : p.whole_ml;
+        o = is_short ? p.part_o : is_long ? p.long_o : p.whole_o;
+        room = is_short ? p.parts_short : is_long ? p.parts_long : 2 * p.g.most_rows * p.heads;
+        by = is_short ? 2 << p.short_shift : p.c.n_heads * kLongTile;
+        n = !room ? 0 : is_short || is_long ? min(max(f.z, 1), 4096) : 1;
+        first = f.x;
+        second = f.y;
+    }
+
+    __device__ int64_t at(int c) const { return min((unsigned)(c == 0 ? first : second + (c - 1) * by), room - 1u); }
+};
 
 // Joins the parts of short tiles that lie across the ends of workgroups' stretches: a workgroup per such end, the first
 // one inside a tile does it.  Workgroups from join_blocks on, join_long of them: the rows of cut long tiles, a wave per row and head.  Where
@@ -502,7 +511,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         for (int row = blockIdx.y * 4 + wave; row < rows; row += 4 * gridDim.y) {
             const int r = (pl.tile << p.short_shift) + row, i = r / p.group_div;
             RowSum x;
-            join_add<DP>(p, x, p.part_ml, p.part_o, n, [&](int c) { return short_part(p, b, c, pl.start, share, row); });
+            const auto part = [&](int c) { return short_part(p, b, c, pl.start, share, row); };
+            join_add<DP>(p, x, n, [&](int c) { return p.part_ml + part(c) * 2; }, [&](int c) { return p.part_o + part(c) * p.c.dim; });
             join_store<DP>(p, x, q.row0 + i, pl.head * p.group + r - i * p.group);
         }
         return;
@@ -512,11 +522,11 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
     if (S && block >= p.join_long) {
         const int n = plan[kGroupRows] * p.heads;
         for (int u = (block - p.join_long) * 4 + wave; u < n; u += (gridDim.x - p.join_blocks - p.join_long) * 4) {
-            const int4 a = p.found[u], b = p.found[u + p.g.most_rows * p.heads];
+            const Found a(p, p.found[u]), b(p, p.found[u + p.g.most_rows * p.heads]);
             const int v = u / p.heads_div, t = min((unsigned)p.g.rows[v], (unsigned)p.b.n_rows - 1u);
             RowSum x;
-            join_found<DP>(p, x, a);
-            join_found<DP>(p, x, b);
+            join_add<DP>(p, x, a.n + b.n, [&](int c) { return c < a.n ? a.ml + a.at(c) * 2 : b.ml + b.at(c - a.n) * 2; },
+                         [&](int c) { return c < a.n ? a.o + a.at(c) * p.c.dim : b.o + b.at(c - a.n) * p.c.dim; });
             join_store<DP>(p, x, t, u - v * p.heads);
         }
         return;
@@ -535,8 +545,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         if (cuts == 1 || (S && whole_at<S>(p, q, s, i) >= 0)) continue;
         const int slot = slots[s] + tile * splits_of(reach_of<kLong>(p, q), chunk) * p.c.n_heads + head;
         RowSum x;
-        join_add<DP>(p, x, p.long_ml, p.long_o, cuts,
-                     [&](int c) { return (int64_t)(slot + c * p.c.n_heads) * kLongTile + r - tile * kLongTile; });
+        const auto part = [&](int c) { return (int64_t)(slot + c * p.c.n_heads) * kLongTile + r - tile * kLongTile; };
+        join_add<DP>(p, x, cuts, [&](int c) { return p.long_ml + part(c) * 2; }, [&](int c) { return p.long_o + part(c) * p.c.dim; });
         join_store<DP>(p, x, q.row0 + i, qh);
     }
 }
