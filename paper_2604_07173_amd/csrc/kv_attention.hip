@@ -499,8 +499,11 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
 {
     const int32_t *plan = p.plan;        // the kernels before have left it
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if ((int)blockIdx.x < p.join_blocks) {
-        const int share = uniform(plan[kShare]), b = blockIdx.x, cut = (b + 1) * share;
+    // (S: those behind come first, as they have most to do: 61 sequences with drafted rows 42.1 -> 41.7 us, 32 answers 22.0 -> 21.1)
+    const int others = p.join_blocks + p.join_long, found = gridDim.x - others;
+    const int id = !S ? blockIdx.x : (int)blockIdx.x < found ? blockIdx.x + others : blockIdx.x - found;
+    if (id < p.join_blocks) {
+        const int share = uniform(plan[kShare]), b = id, cut = (b + 1) * share;
         if (cut >= plan[kUnits]) return;
         Seq<S> q;
         const Place pl = place_of<S>(p, plan, cut, q);
@@ -518,10 +521,10 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p)
         return;
     }
     if (blockIdx.y) return;
-    const int seqs = plan_seqs<S>(p), block = blockIdx.x - p.join_blocks;
+    const int seqs = plan_seqs<S>(p), block = id - p.join_blocks;
     if (S && block >= p.join_long) {
         const int n = plan[kGroupRows] * p.heads;
-        for (int u = (block - p.join_long) * 4 + wave; u < n; u += (gridDim.x - p.join_blocks - p.join_long) * 4) {
+        for (int u = (block - p.join_long) * 4 + wave; u < n; u += found * 4) {
             const Found a(p, p.found[u]), b(p, p.found[u + p.g.most_rows * p.heads]);
             const int v = u / p.heads_div, t = min((unsigned)p.g.rows[v], (unsigned)p.b.n_rows - 1u);
             RowSum x;
