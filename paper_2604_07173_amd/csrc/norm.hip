@@ -44,13 +44,13 @@ __device__ inline void store8(uint16_t *p, const float (&x)[8])
     st16<false>(p, o);
 }
 
-// Over the threads of a row: a wave's lanes, or all waves of the workgroup through LDS.
-template <bool WAVE, class V, class Op>
+// Over the threads of a row: LANES neighbouring lanes of a wave, or, 0, all waves of the workgroup through LDS.
+template <int LANES, class V, class Op>
 __device__ inline V over_row(V v, V *s_part, Op op)
 {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) v = op(v, __shfl_xor(v, d));
-    if (WAVE) return v;
+    for (int d = (LANES ? LANES : 64) / 2; d; d >>= 1) v = op(v, __shfl_xor(v, d));
+    if (LANES) return v;
     __syncthreads();                      // a former call's parts have been read
     if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -61,15 +61,15 @@ __device__ inline V over_row(V v, V *s_part, Op op)
 
 enum Add { kNone, kBf16, kF32 };
 
-// N vectors of a row per thread.  WAVE: a row is a wave's, and a workgroup takes four at a time; otherwise all of it takes one.
-template <bool XF32, Add A, bool WAVE, int N>
-__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormParams p)
+// N vectors of a row per thread.  LANES: a row is that many lanes', and a workgroup takes 256 / LANES at a time; 0: all of it takes one.
+template <bool XF32, Add A, int LANES, int N>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void norm_kernel(NormParams p)
 {
-    constexpr int ROWS = WAVE ? 4 : 1;
+    constexpr int SHARE = LANES ? LANES : 256, ROWS = 256 / SHARE;
     __shared__ float s_part[16];
     __shared__ unsigned s_top[16];
-    const int T = WAVE ? 64 : blockDim.x, t = WAVE ? threadIdx.x & 63 : threadIdx.x;
-    for (int64_t row = WAVE ? (int64_t)blockIdx.x * ROWS + (threadIdx.x >> 6) : blockIdx.x; row < p.n_rows; row += (int64_t)gridDim.x * ROWS) {
+    const int T = LANES ? LANES : blockDim.x, t = LANES ? threadIdx.x % SHARE : threadIdx.x;
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + (LANES ? threadIdx.x / SHARE : 0); row < p.n_rows; row += (int64_t)gridDim.x * ROWS) {
         float s[N][8];
         float sum = 0.f;
 #pragma unroll
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormParams p)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += s[k][i] * s[k][i];
         const auto plus = [](float a, float b) { return a + b; };
-        sum = over_row<WAVE>(sum, s_part, plus);
+        sum = over_row<LANES>(sum, s_part, plus);
         if (p.sum) {
 #pragma unroll
             for (int k = 0; k < N; ++k) {
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormParams p)
                     s[k][i] *= kShrink;
                     sum += s[k][i] * s[k][i];
                 }
-            sum = over_row<WAVE>(sum, s_part, plus);
+            sum = over_row<LANES>(sum, s_part, plus);
             eps = 0.f;                    // far below the mean's last bit
         }
         const float r = 1.f / sqrtf(sum / (float)p.width + eps);
@@ -153,9 +153,9 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormParams p)
         if (p.group) {
 #pragma unroll
             for (int k = 0; k < N; ++k)
-                for (int d = 1; d < p.group >> 3; d <<= 1) tops[k] = max(tops[k], (unsigned)__shfl_xor((int)tops[k], d));
+                for (int d = 1; d < min(p.group >> 3, LANES ? LANES : 64); d <<= 1) tops[k] = max(tops[k], (unsigned)__shfl_xor((int)tops[k], d));
         } else {
-            top = over_row<WAVE>(top, s_top, [](unsigned a, unsigned b) { return max(a, b); });
+            top = over_row<LANES>(top, s_top, [](unsigned a, unsigned b) { return max(a, b); });
 #pragma unroll
             for (int k = 0; k < N; ++k) tops[k] = top;
         }
@@ -187,20 +187,24 @@ template <bool XF32, Add A>
 void launch_width(const NormParams &p, hipStream_t s)
 {
     const int vecs = p.width / 8;
-    // As many waves as the row fills, so that few lanes have nothing to do.  One vector a thread up to five waves (1333 rows of 2056 fp32 columns
+    // As many lanes or waves as the row fills, so that few have nothing to do (20000 rows of 64 columns in bf16 and e4m3 4.8 us, a wave for
+    // each 12.0; of 256 10.5 and 11.9).  One vector a thread up to five waves (1333 rows of 2056 fp32 columns
     // 11.0 us, with two 11.4); with eight 16384 rows of 4096 columns gain 2 % and 2130 of 3912 lose 12
-#define LORA_NORM(WAVE, N)                                                                                     \
+#define LORA_NORM(LANES, N)                                                                                    \
     {                                                                                                          \
-        const int rows = WAVE ? 4 : 1, threads = WAVE ? 256 : (vecs + 64 * N - 1) / (64 * N) * 64;             \
+        const int rows = 256 / (LANES ? LANES : 256), threads = LANES ? 256 : (vecs + 64 * N - 1) / (64 * N) * 64; \
         const int grid = std::min((p.n_rows + rows - 1) / rows, 65536);                                        \
-        hipLaunchKernelGGL((norm_kernel<XF32, A, WAVE, N>), dim3(grid), dim3(threads), 0, s, p);               \
+        hipLaunchKernelGGL((norm_kernel<XF32, A, LANES, N>), dim3(grid), dim3(threads), 0, s, p);              \
     }
-    if (vecs <= 64) LORA_NORM(true, 1)
-    else if (vecs <= 128) LORA_NORM(true, 2)
-    else if (vecs <= 320) LORA_NORM(false, 1)
-    else if (vecs <= 1024) LORA_NORM(false, 2)
-    else if (vecs <= 4096) LORA_NORM(false, 4)
-    else LORA_NORM(false, 8)
+    if (vecs <= 8) LORA_NORM(8, 1)
+    else if (vecs <= 16) LORA_NORM(16, 1)
+    else if (vecs <= 32) LORA_NORM(32, 1)
+    else if (vecs <= 64) LORA_NORM(64, 1)
+    else if (vecs <= 128) LORA_NORM(64, 2)
+    else if (vecs <= 320) LORA_NORM(0, 1)
+    else if (vecs <= 1024) LORA_NORM(0, 2)
+    else if (vecs <= 4096) LORA_NORM(0, 4)
+    else LORA_NORM(0, 8)
 #undef LORA_NORM
 }
 

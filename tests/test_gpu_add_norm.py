@@ -128,6 +128,25 @@ def test_in_place(W):
     check(call(x, a, w, total=False, out_to=x), want)
 
 
+@pytest.mark.parametrize("W", [8, 56, 64, 72, 128, 136, 256, 264])
+@pytest.mark.parametrize("R", [1, 7, 33, 1001])
+def test_rows_that_share_a_wave(R, W):
+    """Each by itself, one that is scaled and one that is no number among them."""
+    for group in (None, 0, 8, 64, 512):
+        x, a, w = make(R, W, f32=True, add="f32")
+        if R > 1:
+            x[R // 2] *= 1e25
+            a[R // 2] *= 1e25
+            x[R // 3, 5] = math.nan
+        good = torch.ones(R, dtype=torch.bool)
+        good[R // 3] = R == 1
+        s, y, y8, scale = call(x, a, w, group)
+        ws, wy = formula(x, a, w, 1e-5, 0.0)
+        pick = lambda v: None if v is None else v[good.to(v.device)]                        # noqa: E731
+        check((pick(s), pick(y), pick(y8), pick(scale)), (pick(ws), pick(wy)), group)
+        assert y[~good.cuda()].isnan().all()
+
+
 def test_results_do_not_depend_on_other_rows_and_repeat():
     x, a, w = make(300, 4096)
     s, y, y8, scale = call(x, a, w, group=128)
