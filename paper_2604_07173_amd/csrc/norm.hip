@@ -187,8 +187,8 @@ template <bool XF32, Add A>
 void launch_width(const NormParams &p, hipStream_t s)
 {
     const int vecs = p.width / 8;
-    // As many lanes or waves as the row fills, so that few have nothing to do (20000 rows of 64 columns in bf16 and e4m3 4.8 us, a wave for
-    // each 12.0; of 256 10.5 and 11.9).  One vector a thread up to five waves (1333 rows of 2056 fp32 columns
+    // As many lanes or waves as the row fills, so that few have nothing to do (20000 rows of 64 columns in bf16 and e4m3 4.8 to 5.6 us, a wave
+    // for each 11.9; of 128 6.7 and 12.4, of 256 10.5 and 13.4).  One vector a thread up to five waves (1333 rows of 2056 fp32 columns
     // 11.0 us, with two 11.4); with eight 16384 rows of 4096 columns gain 2 % and 2130 of 3912 lose 12
 #define LORA_NORM(LANES, N)                                                                                    \
     {                                                                                                          \
