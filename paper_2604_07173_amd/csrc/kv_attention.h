@@ -272,6 +272,9 @@ __device__ inline float group_work(const AttnParams &p, const Seq<true> &q)
     return q.group && n > p.group_limit ? (float)n * (float)q.len * (float)p.c.n_heads : 0.f;
 }
 
+// Groups whose rows are more than there are, each of which is in one group at most, take no part: the sums of their work may not fit 32 bits.
+__device__ inline bool rows_untrue(const AttnParams &p, float rows) { return rows > (float)p.g.most_rows * 1.001f; }
+
 // The plan of up to 64 * MOST sequences, by one wave: lane l takes the sequences l * each .. of the batch.
 template <bool S, int MOST>
 __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
@@ -291,10 +294,14 @@ __device__ inline void make_plan(const AttnParams &p, int32_t *plan)
     }
     int group_limit = p.group_limit;
     if constexpr (S) {
-        float all = 0.f;
+        float all = 0.f, rows = 0.f;
 #pragma unroll
-        for (int k = 0; k < MOST; ++k) all += group_work(p, q[k]);
+        for (int k = 0; k < MOST; ++k) all += group_work(p, q[k]), rows += q[k].group ? (float)q[k].rows : 0.f;
         if (last_lane(wave_scan(all)) <= kGroupsShort) group_limit = INT_MAX;
+        const bool untrue = rows_untrue(p, last_lane(wave_scan(rows)));
+#pragma unroll
+        for (int k = 0; k < MOST; ++k)
+            if (q[k].group && untrue) q[k].rows = 0;
     }
     float units = 0.f;
 #pragma unroll

@@ -42,19 +42,31 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
     float work = 0.f, units = 0.f, tiles = 0.f;
     unsigned bad = 0;
     int group_limit = p.group_limit;
+    bool untrue = false;
     if constexpr (S) {
-        float all = 0.f;
-        for (int s = tid; s < p.g.most; s += kPlanThreads) all += group_work(p, seq_of<true>(p, s));
+        float all = 0.f, rows = 0.f;
+        for (int s = tid; s < p.g.most; s += kPlanThreads) {
+            const Seq<S> q = seq_of<S>(p, s);
+            all += group_work(p, q);
+            rows += (float)q.rows;
+        }
         all = wave_scan(all);
-        if (lane == 63) s_work[wave] = all;
+        rows = wave_scan(rows);
+        if (lane == 63) s_work[wave] = all, s_units[wave] = rows;
         __syncthreads();
-        all = 0.f;
-        for (int w = 0; w < WAVES; ++w) all += s_work[w];
-        __syncthreads();                  // s_work is used again
+        all = rows = 0.f;
+        for (int w = 0; w < WAVES; ++w) all += s_work[w], rows += s_units[w];
+        __syncthreads();                  // they are used again
         if (all <= kGroupsShort) group_limit = INT_MAX;
+        untrue = rows_untrue(p, rows);
     }
+    const auto seq = [&](int s) {
+        Seq<S> q = seq_of<S>(p, s);
+        if (S && q.group && untrue) q.rows = 0;
+        return q;
+    };
     for (int s = tid; s < n; s += kPlanThreads) {
-        const Seq<S> q = seq_of<S>(p, s);
+        const Seq<S> q = seq(s);
         bad |= plan_faults_of<S>(p, s);
         work += (float)tiles_of<kLong>(p, q, group_limit) * (float)reach_of<kLong>(p, q);
         if (S) tiles += (float)tiles_of<kLong>(p, q, group_limit);
@@ -75,7 +87,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnParams p)
         const int s = s0 + tid;
         int own[kPlanSums] = {}, upto[kPlanSums];
         if (s < n) {
-            const Seq<S> q = seq_of<S>(p, s);
+            const Seq<S> q = seq(s);
             if (!no_rows) plan_entry(p, q, shift, chunk, group_limit, own);
             store_seq<S>(p.plan, n, s, q);
         }

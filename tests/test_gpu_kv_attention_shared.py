@@ -193,3 +193,69 @@ def test_two_calls_at_once_on_two_streams():
     torch.cuda.synchronize()
     for out, w in zip(outs, want):
         assert torch.equal(out, w)
+
+
+# Groups of more than 32 rows x heads that share K go in long tiles where all of them together are enough work: rows x group x shared tokens x
+# key/value heads above 2.8e6 of such groups
+@pytest.mark.parametrize("heads,kv,dim,width,tokens", [
+    (32, 8, 128, 70, 2000), (16, 8, 64, 100, 2000), (8, 8, 40, 100, 4000), (20, 5, 80, 90, 2100), (8, 4, 256, 100, 4003), (64, 1, 64, 30, 2000), (6, 2, 8, 250, 2000)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_groups_in_long_tiles(heads, kv, dim, width, tokens, causal):
+    assert width * heads * tokens > 2.9e6            # rows x group x heads of K and V: rows x heads
+    rng = np.random.default_rng(width)
+    case = SharedCase([0] * width + [-1, -1], [tokens], [int(i) for i in rng.integers(0, 60, width + 2)], [1] * (width - 1) + [5, 1, 3], heads=heads, kv=kv, dim=dim, seed=dim)
+    check(case, causal=causal)
+
+
+@pytest.mark.parametrize("seqs,prompts,most,prompt_hi", [(300, 2, 1, 4000), (60, 3, 8, 4000), (500, 9, 1, 2000), (40, 1, 40, 2500)])
+def test_long_tiles_among_others(seqs, prompts, most, prompt_hi):
+    """Plans in LDS and in memory, groups in both kinds of tiles, rows of their own in long ones as well."""
+    check(random_case(seqs + most, seqs, prompts, most=most, prompt_hi=prompt_hi, own_hi=60, heads=16, kv=4, dim=64))
+
+
+def test_a_graph_whose_groups_change_their_tiles():
+    """Lengths on both sides of the rule for groups' tiles, in one captured call."""
+    width = 70
+    case = SharedCase([0] * width, [3000], [i % 9 for i in range(width)], [1] * width, heads=32, kv=8, dim=64, seed=6).device()
+    sh = L.KvShared(width, case.T)
+    out = torch.empty((case.T, 2048), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(L.lora_kv_attention_shared_ws_bytes(case.cache, case.batch, sh, 32), dtype=torch.uint8, device="cuda")
+
+    def both():
+        L.lora_kv_share(case.cache, case.batch, sh)
+        L.lora_kv_attention_shared(case.cache, 0, case.batch, sh, case.qd, 2048, 32, out, 2048, None, 0.125, ws)
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    lens = case.batch.seq_len.clone()
+    for most in (4000, 700, 2990, 40, 4000):         # 70 x 32 x 1250 is the border
+        case.batch.seq_len.copy_(lens.clamp(max=most))
+        case.lens = case.batch.seq_len.tolist()
+        out.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_attention(case, (out, None), attention64(case, 0.125))
+
+
+def test_untrue_groups_in_long_tiles_stay_within_bounds():
+    """As above, with groups whose rows and tokens are as many as the batch has room for."""
+    case = SharedCase([0] * 60 + [-1] * 4, [3000], [5] * 64, [1] * 64, heads=16, kv=4, dim=64, seed=9).device()
+    want = attention64(case, 0.125)
+    lone = torch.arange(60, 64)
+    rng = np.random.default_rng(1)
+    for _ in range(6):
+        sh = share(case)
+        n = int((sh.rows >= 0).sum())
+        wild = rng.choice([-2 ** 31, -1, 0, 7, 60, 3000, 10 ** 6, 2 ** 31 - 1], sh.groups.numel()).astype(np.int32)
+        wild.reshape(-1, 4)[0] = [int(rng.integers(0, 64)), int(rng.choice([2992, 3008, 10 ** 6])), int(rng.integers(0, 9)), int(rng.choice([60, 64, 10 ** 6]))]
+        sh.groups.view(-1).copy_(torch.from_numpy(wild).cuda())
+        sh.rows[:n] = sh.rows[torch.from_numpy(rng.integers(0, n, n)).cuda()]
+        sh.own[:60] = torch.from_numpy(rng.choice([1, 16, 2992, 2 ** 31 - 1], 60).astype(np.int32)).cuda()
+        sh.place[:60] = torch.from_numpy(rng.choice([0, 59, 63, 2 ** 31 - 1], 60).astype(np.int32)).cuda()
+        out, _ = attend_shared(case, sh, 0.125)
+        err = (out.double().cpu() - want[0]).abs()[lone]
+        assert (err <= want[2][lone] * (1.02 * 2.0 ** -7) + 1e-37).all()
+    torch.cuda.synchronize()
