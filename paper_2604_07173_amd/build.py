@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(PKG_DIR, "liblora.so")
 PYCALL_PATH = os.path.join(PKG_DIR, "_pycall.so")           # the binding's argument conversion (csrc/pycall.cpp)
 SOURCES = ["api.hip", "pack.hip", "segments.hip", "segments_large.hip", "shrink.hip", "expand.hip",
            "shrink_decode.hip", "expand_decode.hip", "fused_decode.hip", "combine.hip", "kv_api.hip", "kv_append.hip", "kv_attention.hip", "kv_attention_long.hip", "kv_pages.hip", "kv_share.hip", "step_api.hip", "norm.hip", "sample.hip", "provision.cpp"]
-HEADERS = ["lora_internal.h", "adapter_ranks.h", "lora_layout.h", "lora_device.h", "expand_common.h", "expand_item.h", "shrink_wave.h", "segments_common.h", "segments_inline.h", "kv_internal.h", "kv_layout.h", "kv_work.h", "kv_device.h", "kv_attention.h", "step_internal.h", os.path.join("..", "..", "include", "lora.h"),
+HEADERS = ["lora_internal.h", "adapter_ranks.h", "lora_layout.h", "lora_device.h", "expand_common.h", "expand_item.h", "shrink_wave.h", "segments_common.h", "segments_inline.h", "kv_internal.h", "kv_layout.h", "kv_work.h", "kv_device.h", "kv_attention.h", "step_internal.h", "sample_bins.h", os.path.join("..", "..", "include", "lora.h"),
            os.path.join("..", "..", "include", "lora_provision.h"), os.path.join("..", "..", "include", "lora_attn.h"), os.path.join("..", "..", "include", "lora_step.h")]
 
 HIPCC_FLAGS = [

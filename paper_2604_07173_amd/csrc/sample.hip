@@ -26,6 +26,7 @@
 #include <type_traits>
 
 #include "kv_device.h"
+#include "sample_bins.h"
 #include "step_internal.h"
 
 namespace lora {
@@ -58,21 +59,21 @@ __device__ inline unsigned key_of(float l)
 
 __device__ inline float of_key(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
 
-// A row as 16-byte pieces of memory, four or eight logits each; it begins `skew` logits into the first.
+// A row as 16-byte pieces of memory, four or eight logits each.
 template <bool F32>
-struct Row {
+struct Row : Pieces<F32 ? 4 : 8> {
     static constexpr int VEC = F32 ? 4 : 8, SIZE = F32 ? 4 : 2;
+    using Pieces<VEC>::skew;
+    using Pieces<VEC>::vocab;
     const char *base;
-    int skew, vocab;
 
-    __device__ Row(const void *logits, int64_t at, int vocab) : vocab(vocab)
+    __device__ Row(const void *logits, int64_t at, int vocab)
     {
         const uintptr_t first = reinterpret_cast<uintptr_t>(logits) + at * SIZE;
         base = reinterpret_cast<const char *>(first & ~(uintptr_t)15);
-        skew = (int)(first & 15) / SIZE;
+        this->skew = (int)(first & 15) / SIZE;
+        this->vocab = vocab;
     }
-
-    __device__ int pieces() const { return (skew + vocab + VEC - 1) / VEC; }
 
     // Piece i; -inf, which is never chosen, in place of what is not the row's.
     __device__ u32x4 load(int i) const
@@ -104,9 +105,6 @@ struct Row {
         return __uint_as_float(F32 ? *(const LORA_GLOBAL unsigned *)at : (unsigned)*(const LORA_GLOBAL uint16_t *)at << 16);
     }
 
-    // The number of a piece's logit e.
-    __device__ int number(int i, int e) const { return i * VEC - skew + e; }
-
     // Logit e of a piece.
     static __device__ float at(u32x4 v, int e)
     {
@@ -120,7 +118,6 @@ struct Weigh {
     double top;
     double per, far;                      // 1024 log2(e) / T, and a difference at which the weight is 2^-60
     double least;                         // min_p, in multiples of 2^-shift
-    float top_l;
     int shift;
 
     // The weight of a finite logit, in multiples of 2^-shift, with its fraction.  Without branches, so that several are formed
@@ -144,28 +141,6 @@ struct Weigh {
     {
         const double w = scaled(l);
         return w >= least ? whole(w) : 0;
-    }
-
-    // A number of bins over powers of two of weights.
-    struct Bins {
-        float each;                       // to a logit
-        int most;
-    };
-
-    // Rises as l falls; `most` behind the last bin, and for what is no number.
-    __device__ int bin(float l, Bins b) const { return (int)fminf((top_l - l) * b.each, (float)b.most); }
-
-    // One bin, as the differences that it has; behind the last one, whatever is not below its end.
-    struct Bin {
-        float each, begin, end;
-    };
-    static __device__ Bin only(Bins b, int which) { return {b.each, (float)which, which == b.most ? NAN : (float)(which + 1)}; }
-
-    // (no branches: & in place of &&)
-    __device__ bool is_in(float l, Bin b) const
-    {
-        const float x = (top_l - l) * b.each;
-        return !(x < b.begin) & !(x >= b.end);
     }
 };
 
@@ -359,12 +334,11 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
     Weigh weigh;
     weigh.table = sh.table;
     weigh.top = top;
-    weigh.top_l = top;
     weigh.per = kTable * 1.4426950408889634074 / (double)T;
     weigh.far = -60.0 * kTable / weigh.per;
     weigh.least = min_p > 0.f ? __builtin_ldexp((double)fminf(min_p, 1.f), p.shift) : 0.0;
     weigh.shift = p.shift;
-    const Weigh::Bins by_weight{BINS / 32.f * (1.44269504f / T), BINS}, by_number{COUNTS / 48.f * (1.44269504f / T), COUNTS};
+    const Bins by_weight{BINS / 32.f * (1.44269504f / T), BINS}, by_number{COUNTS / 48.f * (1.44269504f / T), COUNTS};
     const float at_u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
     const auto goal_of = [&](u64 total) { return min((u64)((double)at_u * (double)total), total - 1); };
     const auto chosen = [&](int i, float l, u64 total) {
@@ -387,7 +361,8 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
         for (int w = 0; w < WAVES; ++w) x += sh.wave_mass[w];
         return x;
     };
-    // Lists the tokens for which f holds; their number, which may be more than the list takes, and the range of their keys.
+    // Lists the tokens for which f holds; their number, which may be more than the list takes, and the range of their keys.  f holds for
+    // nothing that is -inf: so only the row's own logits are listed.
     const auto list = [&](auto dense, auto f, unsigned &lo, unsigned &hi) {
         __syncthreads();
         if (tid == 0) sh.listed = 0, sh.lo = 0xFFFFFFFFu, sh.hi = 0;
@@ -543,7 +518,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
             for (int i = tid; i < COUNTS; i += THREADS) sh.count[i] = 0;
             __syncthreads();
             each(some, [&](float l, int) {
-                const int b = weigh.bin(l, by_number);
+                const int b = bin_of(top, l, by_number);
                 if (b < COUNTS) atomicAdd(&sh.count[b], 1u);
             });
             __syncthreads();
@@ -557,12 +532,12 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
         if (!in_list && (sh.bin >= 0 || useless)) {
             const int bin = sh.bin < 0 ? COUNTS : sh.bin;
             u64 above = sh.before;
-            Weigh::Bin it = weigh.only(by_number, bin);
+            Bin it = only_bin(by_number, bin);
             // if the list takes the bins above as well, no later step needs the row: 64 rows of 128000 with mixed limits 112.5 -> 98.4 us,
             // 300 of 32000 72.2 -> 57.5 (not if the list is an eighth of the row at most: 72.7); small rows lose, one of 4000 17.1 -> 20.7
             const bool whole = bin < COUNTS && above + sh.count[min(bin, COUNTS - 1)] <= (u64)min(Lds::LISTED, p.vocab / kListedOf) && p.vocab > kSmallVocab;
             if (whole) it.begin = -INFINITY, above = 0;
-            const auto in_bin = [=](float l) { return (l >= -INFINITY) & weigh.is_in(l, it); };
+            const auto in_bin = [=](float l) { return is_in(top, l, -INFINITY, it); };
             listed = list(yes, in_bin, lo, hi);
             in_list = whole && listed <= (unsigned)Lds::LISTED;
             // fewer tokens than that where many are no numbers: all are left
@@ -602,7 +577,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float l = Row<F32>::at(v, e0 + e);
-                    const int b = weigh.bin(l, by_weight);
+                    const int b = bin_of(top, l, by_weight);
                     if (!(l > from)) continue;
                     if (b < BINS) atomicAdd(&sh.mass[wave][b], x[e]);
                     else tail += x[e];
@@ -629,8 +604,8 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
             u64 mine_above = 0;
             for (int b = lane; b < bin; b += 64) mine_above += sh.mass[wave][b];
             m = wave_sum64(mine_above);
-            const Weigh::Bin it = weigh.only(by_weight, bin);
-            const auto in_bin = [=](float l) { return (l > from) & weigh.is_in(l, it); };
+            const Bin it = only_bin(by_weight, bin);
+            const auto in_bin = [=](float l) { return is_in(top, l, from, it); };
             listed = list(yes, in_bin, lo, hi);
             border = refine(yes, in_bin, lo, hi, listed, want, before);
             // where min_p is the narrower limit the sums are not those of what is kept

@@ -1,0 +1,44 @@
+"""Sampling where the temperature puts all tokens in one bin, and so in the kernel's list: rows among memory whose values would win if they
+were read, of which a mask leaves as many as the list takes, and more."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_sample import check, us
+
+pytestmark = pytest.mark.gpu
+
+
+def among_others(V, R, left, none, kind, pad, start, seed=0):
+    """R rows of V logits, `none` but for `left` of them, from column `start` of a buffer that holds much larger ones everywhere else."""
+    g = torch.Generator().manual_seed(seed + V + left)
+    x = torch.full((R, V), none)
+    for r in range(R):
+        at = torch.randperm(V, generator=g)[:left]
+        x[r, at] = 2.5 * torch.randn(left, generator=g)
+    wide = torch.full((R + 2, V + pad + start), 90.0, dtype=kind, device="cuda")
+    view = wide[1:-1, start:start + V]
+    view.copy_(x.to(kind))
+    return view
+
+
+# V: of workgroups of 256, 512 and 1024 threads.  left: fewer than a list takes, all of them, and more
+@pytest.mark.parametrize("V,left,k", [(1500, 700, 300), (1500, 1500, 900), (8190, 3000, 1000), (8190, 8190, 5000), (50257, 10000, 3000), (50257, 50257, 20000)])
+@pytest.mark.parametrize("T", [math.inf, 1e-38, 1e-45])
+@pytest.mark.parametrize("kind,pad,start", [(torch.float32, 0, 0), (torch.float32, 3, 1), (torch.bfloat16, 5, 3)])
+def test_one_bin_of_all_tokens(V, left, k, T, kind, pad, start):
+    for none in (-math.inf, math.nan):
+        x = among_others(V, 5, left, none, kind, pad, start)
+        check(x, T=T, k=k, u=us(5))
+        check(x, T=T, k=k, p=0.7, u=us(5, 1))
+        check(x, T=T, k=k, least=0.5, u=us(5, 2))
+
+
+def test_the_last_row_of_a_buffer():
+    """Nothing behind it."""
+    for V in (1000, 16388):
+        x = torch.empty(V, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(V))[None]
+        for T in (math.inf, 1e-38):
+            check(x, T=T, k=V - 7, u=us(1))
