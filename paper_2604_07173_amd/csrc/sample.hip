@@ -338,7 +338,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
     weigh.far = -60.0 * kTable / weigh.per;
     weigh.least = min_p > 0.f ? __builtin_ldexp((double)fminf(min_p, 1.f), p.shift) : 0.0;
     weigh.shift = p.shift;
-    const Bins by_weight{BINS / 32.f * (1.44269504f / T), BINS}, by_number{COUNTS / 48.f * (1.44269504f / T), COUNTS};
+    const Bins by_weight = bins_over(32.f, BINS, T), by_number = bins_over(48.f, COUNTS, T);
     const float at_u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
     const auto goal_of = [&](u64 total) { return min((u64)((double)at_u * (double)total), total - 1); };
     const auto chosen = [&](int i, float l, u64 total) {

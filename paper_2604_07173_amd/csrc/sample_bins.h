@@ -22,12 +22,17 @@ struct Pieces {
 
 // A number of bins over powers of two of weights.
 struct Bins {
-    float each;                           // to a logit
+    float each;                           // to half a difference of logits
     int most;
 };
 
+LORA_HD Bins bins_over(float powers, int most, float T) { return Bins{(float)most / powers * (1.44269504f / T) * 2.f, most}; }
+
+// Half of what l is below the largest logit, with one rounding, as the whole: that may be beyond a float where T is as large.
+LORA_HD float half_below(float top, float l) { return fmaf(l, -0.5f, top * 0.5f); }
+
 // Rises as l falls; `most` behind the last bin, and for what is no number.
-LORA_HD int bin_of(float top, float l, Bins b) { return (int)fminf((top - l) * b.each, (float)b.most); }
+LORA_HD int bin_of(float top, float l, Bins b) { return (int)fminf(half_below(top, l) * b.each, (float)b.most); }
 
 // One bin, as the differences that it has; behind the last one, whatever is not below its end.
 struct Bin {
@@ -40,7 +45,7 @@ LORA_HD Bin only_bin(Bins b, int which) { return Bin{b.each, (float)which, which
 // temperature makes `each` zero or infinite, and -inf is what stands in front of a row and behind it.  (no branches: & in place of &&)
 LORA_HD bool is_in(float top, float l, float from, Bin b)
 {
-    const float x = (top - l) * b.each;
+    const float x = half_below(top, l) * b.each;
     return (l > from) & !(x < b.begin) & !(x >= b.end);
 }
 

@@ -42,3 +42,20 @@ def test_the_last_row_of_a_buffer():
         x = torch.empty(V, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(V))[None]
         for T in (math.inf, 1e-38):
             check(x, T=T, k=V - 7, u=us(1))
+
+
+@pytest.mark.parametrize("V", [3, 40, 3000, 20000])
+@pytest.mark.parametrize("T", [1e38, 2e38, math.inf])
+def test_tokens_further_below_than_floats_reach(V, T):
+    """Several of them, of weights that count."""
+    x = torch.full((3, V), -math.inf)
+    x[:, [0, V // 2, V - 1]] = torch.tensor([-3.2e38, 3e38, -3e38])
+    if V > 3:
+        x[1:, 1:4] = torch.tensor([-2.5e38, 1e38, -3.1e38])
+        x[2, 4:V // 2] = torch.linspace(-3.3e38, -1e38, V // 2 - 4)
+    x = x.cuda()
+    for k in (1, 2, 3, 4, 5, 700, 2000):
+        check(x, T=T, k=k, u=us(3, k))
+        check(x, T=T, k=k, p=0.9, u=us(3, k))
+        check(x, T=T, k=k, least=0.1, u=us(3, k))
+    check(x, T=T, p=0.95, u=us(3))

@@ -40,7 +40,7 @@ void run(int threads, int skew, float T, unsigned want, const std::vector<float>
     float top = -INFINITY;
     for (float x : l) top = fmaxf(top, x);
     const int most = 4 * threads;
-    const lora::Bins bins{most / 48.f * (1.44269504f / T), most};
+    const lora::Bins bins = lora::bins_over(48.f, most, T);
     std::vector<unsigned> count(most);
     each<VEC>(threads, skew, l, [&](float x, int) {
         const int b = lora::bin_of(top, x, bins);
@@ -106,3 +106,18 @@ def test_only_tokens_of_the_row_are_listed(listed, V, threads, vec, T):
                 if T in (math.inf, 1e-45, 1e-38):
                     assert len(numbers) == len(real) and bin == (0 if T == math.inf else 4 * threads)
                 assert numbers
+
+
+@pytest.mark.parametrize("T", [math.inf, 3e38, 2e38, 1e37, 1.0])
+def test_no_token_with_a_weight_is_behind_the_bins(listed, T):
+    """Also where the difference of two logits is infinite in 32 bits: the bin of the k-th token is found, and no token that stands after all
+    of its values is in it."""
+    rng = np.random.default_rng(3)
+    few = np.array([3e38, -3e38, -3.2e38, -1e38, 3.3e38, -3.4e38, 0.0], np.float32)
+    for l in (few[:3], few, (3.4e38 * rng.uniform(-1, 1, 500)).astype(np.float32)):
+        order = np.argsort(-l.astype(np.float64), kind="stable")
+        weight = np.exp((l.astype(np.float64) - np.float64(l.max())) / np.float64(np.float32(T)))
+        for k in range(1, len(l) + 1):
+            bin, numbers = listed(l, 4, 256, 1, T, k)
+            if weight[order[k - 1]] >= 2.0 ** -47:           # of less it is less than half of what weights are multiples of
+                assert bin < 1024 and order[k - 1] in numbers, (k, bin, numbers)
