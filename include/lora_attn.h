@@ -172,7 +172,8 @@ int lora_kv_attention(const lora_kv_cache *cache, int layer, const lora_kv_batch
  *   own[s]    shared tokens of s's group, 0 if in none;  place[s]: the entry of s's first new row in rows, or -1
  *   counts    groups, their rows, their members, and tokens that need not be read again (at most 2^31 - 1)
  * A length that makes no sense raises LORA_STATUS_BAD_LENGTH in the batch's status word and its sequence takes no part; rows that are no
- * partition raise it too, and there is no group then.  One launch for small batches, else three.  The result holds for all layers
+ * partition raise it too, and there is no group then.  A batch without rows (n_rows 0) has nothing to share, which the host knows: the
+ * call does nothing then, and groups, rows, own, place and counts stay those of the call before.  One launch for small batches, else three.  The result holds for all layers
  * of a step.  It may also be written by other means, as long as it says the truth.
  *
  * lora_kv_attention_shared is lora_kv_attention without a window for a batch with its groups: a group's shared tokens are

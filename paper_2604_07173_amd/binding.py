@@ -731,6 +731,7 @@ class KvShared:
 
 
 def lora_kv_share(cache: KvCache, batch: KvBatch, shared: KvShared, min_pages: int = 1, max_rows: int = 0, stream=None):
+    """Fills shared's tensors; a batch without rows leaves them as they are."""
     rc = _calls().kv_share(cache, batch, shared, min_pages, max_rows, stream)
     if rc:
         _check(rc, "lora_kv_share")

@@ -121,3 +121,14 @@ def test_another_stream_and_repeated_calls_in_a_graph():
     L.lora_kv_share(case.cache, case.batch, got, stream=side)
     side.synchronize()
     assert torch.equal(got.groups, want.groups) and torch.equal(got.rows, want.rows)
+
+
+def test_a_batch_without_rows_leaves_the_results_of_the_call_before():
+    case = random_case(3, 20, 2, most=1, prompt_hi=200, heads=1, kv=1, dim=8).device()
+    want, sh = share(case), share(case)
+    none = L.KvBatch(torch.zeros_like(case.batch.row_start), case.batch.seq_len, case.batch.table, n_rows=0)
+    L.lora_kv_share(case.cache, none, sh)
+    torch.cuda.synchronize()
+    assert int(sh.counts[0]) > 0 and int(none.status) == 0
+    for name in ("groups", "rows", "own", "place", "counts"):
+        assert torch.equal(getattr(sh, name), getattr(want, name))
