@@ -29,7 +29,7 @@ enum {
  * dtype: LORA_DTYPE_BF16 or LORA_DTYPE_F32.  add NULL: s = x.  sum, out, out8: NULL if not wanted, one at least is.
  * Rows are row-major, their strides in elements and multiples of 8.  sum and out may be x or add itself where the element types
  * and strides are the same; other overlaps are not allowed.  Squares that are beyond fp32 are not lost: a row is scaled first if
- * their sum is infinite.  A NaN or an infinity in s makes its row's y NaN, or 0 where only others are infinite.
+ * their sum, or their mean with eps, is infinite.  A NaN or an infinity in s makes its row's y NaN, or 0 where only others are infinite.
  *
  * out8: values in e4m3 (4 exponent bits, 3 of mantissa, largest value 448, no infinities).  The columns of a row are cut into groups of
  * `group` (a power of two, 8 .. 512, the last group may be shorter; 0: the whole row); each has a scale, the largest |y| over 448,

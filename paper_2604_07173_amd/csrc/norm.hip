@@ -16,7 +16,7 @@ namespace lora {
 namespace {
 
 constexpr float kMost8 = 448.f;           // largest e4m3 value
-constexpr float kShrink = 0x1p-80f;       // rows whose squares' sum is infinite: 65536 (2^128 2^-80)^2 is far below 2^128
+constexpr float kShrink = 0x1p-80f;       // rows whose mean of squares and eps are infinite: 65536 (2^128 2^-80)^2 is far below 2^128
 
 template <bool F32>
 __device__ inline void load8(const void *base, int64_t at, float (&x)[8])
@@ -109,8 +109,8 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void norm_kernel(NormParams p)
             }
         }
         if (!p.out && !p.out8) continue;
-        float eps = p.eps;
-        if (sum == INFINITY) {            // the same for all threads of the row
+        float mean = sum / (float)p.width + p.eps;
+        if (mean == INFINITY) {           // the same for all threads of the row
             sum = 0.f;
 #pragma unroll
             for (int k = 0; k < N; ++k)
@@ -120,9 +120,9 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void norm_kernel(NormParams p)
                     sum += s[k][i] * s[k][i];
                 }
             sum = over_row<LANES>(sum, s_part, plus);
-            eps = 0.f;                    // far below the mean's last bit
+            mean = sum / (float)p.width + p.eps * kShrink * kShrink;
         }
-        const float r = 1.f / sqrtf(sum / (float)p.width + eps);
+        const float r = 1.f / sqrtf(mean);
         unsigned top = 0;                 // of |y| as bits: a NaN is above all numbers
 #pragma unroll
         for (int k = 0; k < N; ++k) {
