@@ -25,7 +25,8 @@ enum {
  * Residual and norm.  Row by row, in fp32:
  *   s = x + add,   r = 1 / sqrt(mean of s^2 + eps),   y = s * r * (weight + shift)
  * sum receives s, in x's type, out y in bf16, out8 y in 8 bits with scales (the product of a base weight in 8 bits takes
- * these, the adapters' products the bf16 rows); each is rounded once, to nearest even.  x_dtype, add_dtype and the weights'
+ * these, the adapters' products the bf16 rows); each is rounded once, to nearest even (values in 8 bits
+ * from their quotient with the scale in fp32).  x_dtype, add_dtype and the weights'
  * dtype: LORA_DTYPE_BF16 or LORA_DTYPE_F32.  add NULL: s = x.  sum, out, out8: NULL if not wanted, one at least is.
  * Rows are row-major, their strides in elements and multiples of 8.  sum and out may be x or add itself where the element types
  * and strides are the same; other overlaps are not allowed.  Squares that are beyond fp32 are not lost: a row is scaled first if

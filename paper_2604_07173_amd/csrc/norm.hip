@@ -165,13 +165,18 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void norm_kernel(NormParams p)
             if (c >= p.width) continue;
             const float most = __uint_as_float(tops[k]);
             const float scale = most == 0.f ? 1.f : most / kMost8;
-            // 448 / most would be infinite for the smallest
-            const float up = most < 1e-30f ? 0x1p100f : 1.f;
-            const float inv = most == 0.f ? 1.f : kMost8 / (most * up);
+            // y / scale as a product with 1 / scale, and what that leaves of y divided once more: the quotient, rounded once.  Of the smallest
+            // values 2^100 times as much, so that nothing is lost below 2^-126; where the largest is infinite, the first product stands
+            const float up = most < 1e-20f ? 0x1p100f : 1.f;
+            const float by = most * up / kMost8, inv = most == 0.f ? 1.f : 1.f / by, rest_by = most < INFINITY ? by : 0.f;
+            const auto over = [=](float y) {
+                const float a = y * up, q = a * inv;
+                return fmaf(fmaf(-q, rest_by, a), inv, q);
+            };
             int packed[2] = {0, 0};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float a = s[k][2 * i] * up * inv, b = s[k][2 * i + 1] * up * inv;
+                const float a = over(s[k][2 * i]), b = over(s[k][2 * i + 1]);
                 // what rounding has taken beyond the largest value comes back; a NaN stays one
                 const float x = a > kMost8 ? kMost8 : a < -kMost8 ? -kMost8 : a, y = b > kMost8 ? kMost8 : b < -kMost8 ? -kMost8 : b;
                 if (i & 1) packed[i >> 1] = __builtin_amdgcn_cvt_pk_fp8_f32(x, y, packed[i >> 1], true);
