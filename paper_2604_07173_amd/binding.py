@@ -823,20 +823,6 @@ def _holds_floats(t, what, n):
         raise ValueError(f"{what}: a contiguous float32 tensor of {n} elements at least, got {t.dtype} {list(t.shape)}")
 
 
-_torch_types = {}
-
-
-def _is_of(t, what, dtype):
-    """A tensor whose elements are of the type that the call is told; what is no tensor is an address and goes as it is."""
-    if not hasattr(t, "is_contiguous"):
-        return
-    if not _torch_types:
-        import torch
-        _torch_types.update({LORA_DTYPE_BF16: torch.bfloat16, LORA_DTYPE_F32: torch.float32})
-    if t.dtype is not _torch_types.get(dtype, t.dtype):              # other numbers than these two the call refuses by itself
-        raise ValueError(f"{what}: the call is told {_torch_types[dtype]}, got {t.dtype}")
-
-
 class Norm:
     """lora_norm over a weight tensor [width] (bf16 or float32), or without one.  Holds the tensor."""
 
@@ -869,9 +855,8 @@ class Rows8:
 
 def lora_add_norm(norm: Norm, n_rows: int, x, ldx, add, ldadd, total, ldt, out, ldo, out8: Optional[Rows8] = None,
                   x_dtype=LORA_DTYPE_BF16, add_dtype=LORA_DTYPE_BF16, stream=None):
-    """total, out, out8 (None if not wanted) from x + add: the sum in x's type, its norm in bf16 and in 8 bits."""
-    for t, what, dtype in ((x, "x", x_dtype), (add, "add", add_dtype), (total, "total", x_dtype), (out, "out", LORA_DTYPE_BF16)):
-        _is_of(t, what, dtype)
+    """total, out, out8 (None if not wanted) from x + add: the sum in x's type, its norm in bf16 and in 8 bits.  Tensors of another type
+    than the call is told are a ValueError."""
     if isinstance(out8, Rows8) and isinstance(norm, Norm) and (out8.values.shape[0] < n_rows or out8.values.shape[1] != norm.c.width):
         raise ValueError(f"out8: values of {n_rows} rows of {norm.c.width}, got {list(out8.values.shape)}")
     rc = _calls().add_norm(norm, n_rows, x, ldx, x_dtype, add, ldadd, add_dtype, total, ldt, out, ldo, out8, stream)
@@ -894,9 +879,9 @@ class Sampling:
 
 
 def lora_sample(logits, ld, n_rows: int, vocab: int, how: Sampling, u, token, prob=None, dtype=LORA_DTYPE_F32, stream=None):
+    """Logits that are a tensor of another type than dtype are a ValueError."""
     if isinstance(how, Sampling) and how.holds < n_rows:
         raise ValueError(f"how: settings of {n_rows} rows, got {how.holds}")
-    _is_of(logits, "logits", dtype)
     _holds_floats(u, "u", n_rows)
     _holds_int32(token, "token", n_rows)
     if prob is not None:

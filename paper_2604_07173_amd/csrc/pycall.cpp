@@ -40,7 +40,7 @@ struct Library {
 // Python-side helpers, set by bind(): the slow but always right way to a stream's handle, and, once
 // torch has initialised the device, the two calls behind torch.cuda.current_stream().
 PyObject *slow_stream, *current_device, *raw_stream;
-PyObject *s_data_ptr, *s_numel, *s_element_size, *s_handle, *s_value, *s_c, *s_ws;
+PyObject *s_data_ptr, *s_dtype, *s_numel, *s_element_size, *s_handle, *s_value, *s_c, *s_ws;
 
 bool to_u64(PyObject *v, uint64_t &out)            // a Python int: an address or a size
 {
@@ -64,6 +64,33 @@ bool addr(PyObject *v, void *&out)
     if (v != Py_None && !(PyLong_Check(v) ? to_u64(v, a) : call_u64(v, s_data_ptr, a))) return false;
     out = reinterpret_cast<void *>(a);
     return true;
+}
+
+// the same of a tensor whose elements are of type `dtype`, as the call is told: of another one they would be read to another length.  An
+// int says nothing of its elements, and numbers that are no type the call refuses by itself
+bool addr_of(PyObject *v, int dtype, const char *what, void *&out)
+{
+    if (!addr(v, out)) return false;
+    if (v == Py_None || PyLong_Check(v) || (dtype != LORA_DTYPE_BF16 && dtype != LORA_DTYPE_F32)) return true;
+    PyObject *type = PyObject_GetAttr(v, s_dtype);
+    if (!type) {                                    // no tensor
+        if (!PyErr_ExceptionMatches(PyExc_AttributeError)) return false;
+        PyErr_Clear();
+        return true;
+    }
+    static PyObject *types[2];
+    if (!types[1]) {                                // whoever has a tensor has torch
+        PyObject *torch = PyImport_ImportModule("torch");
+        if (torch) {
+            types[0] = PyObject_GetAttrString(torch, "bfloat16");
+            types[1] = types[0] ? PyObject_GetAttrString(torch, "float32") : nullptr;
+            Py_DECREF(torch);
+        }
+    }
+    const bool ok = types[1] && type == types[dtype == LORA_DTYPE_F32];
+    if (!ok && types[1]) PyErr_Format(PyExc_ValueError, "%s: the call is told %S, got %S", what, types[dtype == LORA_DTYPE_F32], type);
+    Py_DECREF(type);
+    return ok;
 }
 
 bool to_int(PyObject *v, int &out)
@@ -465,9 +492,9 @@ LORA_PY(add_norm)
     int rows, xt, at;
     void *x, *add, *sum, *out, *st;
     int64_t ldx, lda, lds, ldo;
-    if (!n_args(n, 14) || !structure_or_none(a[0], w, w_ref, "lora_norm") || !to_int(a[1], rows) || !addr(a[2], x) || !to_i64(a[3], ldx) ||
-        !to_int(a[4], xt) || !addr(a[5], add) || !to_i64(a[6], lda) || !to_int(a[7], at) || !addr(a[8], sum) || !to_i64(a[9], lds) ||
-        !addr(a[10], out) || !to_i64(a[11], ldo) || !structure_or_none(a[12], r8, r_ref, "lora_rows8") || !stream_of(a[13], st))
+    if (!n_args(n, 14) || !structure_or_none(a[0], w, w_ref, "lora_norm") || !to_int(a[1], rows) || !to_int(a[4], xt) ||
+        !addr_of(a[2], xt, "x", x) || !to_i64(a[3], ldx) || !to_int(a[7], at) || !addr_of(a[5], at, "add", add) || !to_i64(a[6], lda) ||
+        !addr_of(a[8], xt, "total", sum) || !to_i64(a[9], lds) || !addr_of(a[10], LORA_DTYPE_BF16, "out", out) || !to_i64(a[11], ldo) || !structure_or_none(a[12], r8, r_ref, "lora_rows8") || !stream_of(a[13], st))
         return nullptr;
     LORA_CALL(lib.add_norm(w, rows, x, ldx, xt, add, lda, at, sum, lds, out, ldo, r8, st));
 }
@@ -480,7 +507,7 @@ LORA_PY(sample)
     int type, rows, vocab;
     void *x, *u, *token, *prob, *st;
     int64_t ld;
-    if (!n_args(n, 10) || !addr(a[0], x) || !to_i64(a[1], ld) || !to_int(a[2], type) || !to_int(a[3], rows) || !to_int(a[4], vocab) ||
+    if (!n_args(n, 10) || !to_int(a[2], type) || !addr_of(a[0], type, "logits", x) || !to_i64(a[1], ld) || !to_int(a[3], rows) || !to_int(a[4], vocab) ||
         !structure_or_none(a[5], how, h_ref, "lora_sampling") || !addr(a[6], u) || !addr(a[7], token) || !addr(a[8], prob) ||
         !stream_of(a[9], st))
         return nullptr;
@@ -638,7 +665,7 @@ PyMODINIT_FUNC PyInit__pycall(void)
     struct {
         PyObject **at;
         const char *text;
-    } const names[] = {{&s_data_ptr, "data_ptr"}, {&s_numel, "numel"}, {&s_element_size, "element_size"},
+    } const names[] = {{&s_data_ptr, "data_ptr"}, {&s_dtype, "dtype"}, {&s_numel, "numel"}, {&s_element_size, "element_size"},
                        {&s_handle, "handle"}, {&s_value, "value"}, {&s_c, "c"}, {&s_ws, "ws"}};
     for (const auto &v : names)
         if (!(*v.at = PyUnicode_InternFromString(v.text))) return nullptr;
