@@ -135,7 +135,8 @@ class Answers(Server):
         m, P, state = self.model, tokens.shape[0], self.states[0]
         start = torch.from_numpy(np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)).cuda()
         batch = L.KvBatch(start, state.seq_len, state.table, n_rows=P, max_rows=max(rows))
-        shared = L.KvShared(self.slots, P)
+        # rows of groups: 16 a sequence at most take part, and the attention's workspace has two results for each
+        shared = L.KvShared(self.slots, min(P, 16 * self.slots))
         L.lora_kv_share(self.cache, batch, shared, max_rows=16)
         ids = torch.from_numpy(np.repeat(self.adapter, rows).astype(np.int32)).cuda()
         seg = L.Segments(P)

@@ -175,12 +175,15 @@ int lora_kv_attention(const lora_kv_cache *cache, int layer, const lora_kv_batch
  * partition raise it too, and there is no group then.  A batch without rows (n_rows 0) has nothing to share, which the host knows: the
  * call does nothing then, and groups, rows, own, place and counts stay those of the call before.  One launch for small batches, else three.  The result holds for all layers
  * of a step.  It may also be written by other means, as long as it says the truth.
+ * There is one level of groups: a page that all prompts begin with makes one group of all their answers, which shares that page and
+ * nothing more.  min_pages above the pages that are common to different prompts keeps these apart.
  *
  * lora_kv_attention_shared is lora_kv_attention without a window for a batch with its groups: a group's shared tokens are
  * taken from its leader's table, and the entries for them in the others' tables are not looked at.  Bits may differ from
  * lora_kv_attention's, as sums are taken in another order; they are the same from run to run.  What `shared` says wrongly makes the results of the
  * rows concerned mean nothing, and nothing is read or written out of bounds.  n_rows * n_heads and the same of shared->n_rows: at most 2^26
- * (LORA_ERR_TOO_LARGE).  ws depends on what lora_kv_attention_ws_bytes depends on, and on shared's n_rows and max_group_rows.
+ * (LORA_ERR_TOO_LARGE).  ws depends on what lora_kv_attention_ws_bytes depends on, and on shared's n_rows and max_group_rows: two partial
+ * results in fp32 for every head of every entry of rows, so n_rows should be no larger than lora_kv_share asks for.
  * ------------------------------------------------------------------------------------ */
 typedef struct lora_kv_shared {
     int32_t n_seqs;           /* sequences of the batch */

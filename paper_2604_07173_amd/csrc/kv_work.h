@@ -30,7 +30,8 @@ constexpr int kInlineSeqs = 256;         // sequences up to which every workgrou
 // 32-bit words of the plan in memory: of its head, and of each sequence
 constexpr int kPlanHead = 8, kPlanArrays = 7;
 // The same for batches that share tokens: groups and sequences, with the tokens that each begins at (256 sequences in 16 groups: 124 us; with the
-// plan made in a launch of its own and searched in memory 152; of 64 and fewer a lane takes one each: 8 sequences 14.9 us, otherwise 15.7)
+// plan made in a launch of its own and searched in memory 152; of 64 and fewer a lane takes one each: 8 sequences 14.9 us, otherwise 15.7).
+// So from 257 sequences on there is a launch more, and a search in memory (answers to 32 prompts of 1000 to 3000 tokens: 256 of them 132 us, 257 147, 512 159)
 constexpr int kSharedInline = kInlineSeqs + kInlineSeqs / 2, kSharedArrays = 8;
 
 inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }

@@ -1,8 +1,10 @@
 // The residual's addition and the norm behind it in one pass: s = x + add, y = s r (w + shift) with r = 1 / sqrt(mean s^2 + eps), in
-// fp32.  A row stays in registers between its sum of squares and its outputs, so every element is read once and written once
+// fp32.  A row stays in registers between its sum of squares and its outputs (above 32768 columns partly in scratch memory: 64 of a thread's
+// 128 registers hold it), so every element is read once and written once
 // and the kernel is bound by memory (by latency for a decode batch's few rows): 16384 rows of 4096 columns, bf16, with the residual's sum, the
 // bf16 rows and e4m3 ones with a scale for every 128 columns (606 MB) 117 us, 5.2 TB/s, more than a plain copy of as much (4.85);
-// 1333 rows of 2056 fp32 columns (41 MB) 11 us; 64 rows 4.5 us, of which a launch takes 3.
+// 1333 rows of 2056 fp32 columns (41 MB) 11 us; 64 rows 4.5 us, of which a launch takes 3.  Wide rows, 2048 of them in bf16 with e4m3: 16384 columns
+// 67 us, 4.5 TB/s; 32768 135 us, 4.5; 65536 392 us, 3.1.
 //
 // Vector v of a row, eight columns, belongs to thread v % T of the row's T threads: loads are contiguous over a wave, and a group of
 // columns that share a scale (8 .. 512) lies in neighbouring lanes of one wave.
