@@ -615,10 +615,11 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(SampleParams p)
 
     // 4: the token
     const u64 tie_mass = endless ? (u64)1 << p.shift : border.value > -INFINITY ? weigh.kept(border.value) : 0;
-    // below this, min_p leaves nothing: ln(min_p) T below the largest, and a little more than what the rounding of either may take
+    // below this, min_p leaves nothing: ln(min_p) T below the largest, and a little more than what the rounding of either may take, or that of
+    // a weight: at min_p = 1 all tokens count whose weights are one in 64 bits
     float least_l = border.value;
     if (min_p > 0.f && !endless) {
-        const float far = -logf(fminf(min_p, 1.f)) * T;
+        const float far = (1e-6f - logf(fminf(min_p, 1.f))) * T;
         least_l = fmaxf(least_l, top - far * 1.0001f - (fabsf(top) + far) * 1e-6f);
     }
     // kept tokens of a piece above the border, and those equal to it

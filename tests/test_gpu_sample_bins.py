@@ -59,3 +59,17 @@ def test_tokens_further_below_than_floats_reach(V, T):
         check(x, T=T, k=k, p=0.9, u=us(3, k))
         check(x, T=T, k=k, least=0.1, u=us(3, k))
     check(x, T=T, p=0.95, u=us(3))
+
+
+@pytest.mark.parametrize("V", [40, 3000, 50257])
+@pytest.mark.parametrize("scale,T", [(2.5, 3.3e38), (2.5, math.inf), (1e-20, 1.0), (1e-30, 1e-3), (0.0, 1.0), (1.0, 1e12)])
+def test_weights_that_are_all_one(V, scale, T):
+    """Where every weight is one in 64 bits, min_p = 1 leaves all tokens, wherever the largest stands."""
+    x = (scale * torch.randn((6, V), generator=torch.Generator().manual_seed(V))).cuda()
+    # At T = 1e12 weights are below one, by up to 9 / 1e12: many by less than the 2^-38 = 3.6e-12 that the oracle leaves to the weights' last
+    # bits, so that every row has a list of tokens there
+    unsure = 1.0 if T == 1e12 else 0.02
+    check(x, T=T, least=1.0, u=us(6), most_unsure=unsure)
+    check(x, T=T, least=1.0, k=V // 2, u=us(6, 1), most_unsure=unsure)
+    check(x, T=T, least=1.0, p=0.5, u=us(6, 2), most_unsure=unsure)
+    check(x, T=T, least=1.0 - 2.0 ** -24, u=us(6, 3), most_unsure=unsure)
