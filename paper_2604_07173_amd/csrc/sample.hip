@@ -18,7 +18,7 @@
 //
 // Bound by the instructions that form weights, 24 for each token that has one, four cycles a wave at 64 bits (28 us for 128000 tokens of a
 // row), and by the latency of a pass and of its sums over the workgroup, some 3 us each; the reading comes third.  64 rows of
-// 128000 fp32 logits (33 MB) with limits of their own 90 to 113 us, 512 of 50257 bf16 (51 MB) with top_p = 0.95 69 us, one of 32000 with top_k = 50 and
+// 128000 fp32 logits (33 MB) with limits of their own 82 to 113 us, 512 of 50257 bf16 (51 MB) with top_p = 0.95 69 us, one of 32000 with top_k = 50 and
 // top_p = 0.9 12.5 us, of which a launch takes 3.
 #include <limits.h>
 
